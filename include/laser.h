@@ -256,6 +256,113 @@ int laser_percentiles(const double* values, int32_t n, const double* q, int32_t 
 int laser_summary_f32(const float* values, int32_t n, const double* q, int32_t nq, double* mean,
                       double* out, void* hip_stream);
 
+/*
+ * The experts behind the routing call: the two matrix products of each expert over the
+ * rows that the dispatch tables give it.
+ */
+typedef struct laser_experts_params {
+  uint32_t struct_bytes; /* = sizeof(laser_experts_params_t)                           */
+  int32_t k;             /* experts per token of the tables: slot s belongs to token s / k */
+  int32_t dtype;         /* LASER_DTYPE_* of hidden, the weights, act, base and out    */
+  int32_t first_expert;  /* the call's E experts are first_expert .. first_expert+E-1  */
+                         /* of the tables (0 unless the layer is spread over GPUs);    */
+                         /* the tables themselves are always those of the whole layer  */
+} laser_experts_params_t;
+
+/*
+ * First product and activation:  for every position p of the tables that belongs to one
+ * of the call's experts e, with token t = permutation[p] / k,
+ *   act[p,f] = silu(sum_h hidden[t,h] w_up[e,f,h]) * (sum_h hidden[t,h] w_up[e,F+f,h]),
+ * silu(g) = g / (1 + exp(-g)); sums in fp32, act rounded once to the dtype.
+ *   hidden         [T,H]                                                  in
+ *   w_up           [E,2F,H]: per expert F rows of the gate matrix, then   in
+ *                  F rows of the up matrix
+ *   permutation    [T*k] and expert_offsets [first_expert+E+1 or more]    in
+ *                  from a routing call; both NULL (k = E = 1, first_expert = 0): one
+ *                  expert that takes every token, as a shared expert does, p = t
+ *   act            [T*k,F] in the order of the permutation; rows of positions that    out
+ *                  belong to none of the call's experts are left as they were
+ * Nothing is allocated, no workspace is needed.
+ * Limits (both calls): first_expert + E <= 64, k <= 16, H and F multiples of 8 (bf16) or
+ * 4 (fp32), matrices 16-byte aligned, row-major without gaps.  Tables with entries out of
+ * range give unspecified values, never an access outside the arrays.
+ */
+int laser_experts_up(const void* hidden, const void* w_up, int32_t T, int32_t H, int32_t F,
+                     int32_t E, const laser_experts_params_t* params, const int32_t* permutation,
+                     const int32_t* expert_offsets, void* act, void* hip_stream);
+
+/* Bytes of device workspace laser_experts_down needs (0 on bad arguments); enough for
+ * every call with fewer tokens as well. */
+size_t laser_experts_workspace_bytes(int32_t T, int32_t H, int32_t F, int32_t E,
+                                     const laser_experts_params_t* params);
+
+/*
+ * Second product, weighted and summed back into token order:
+ *   out[t,:] = base[t,:] + sum over the slots s = t*k + j that belong to the call's experts
+ *              of weights[s] * (w_down[e] act[p(s)]),   p(s) the position of slot s,
+ * in slot order, in fp32, rounded once to the dtype.
+ *   act            [T*k,F] from laser_experts_up                          in
+ *   w_down         [E,H,F]                                                in
+ *   permutation, expert_offsets   as above                                in
+ *   expert_ids     [T,k] of the same routing call; NULL: every slot       in
+ *                  belongs to the call's experts
+ *   weights        [T,k] fp32; NULL: 1                                    in
+ *   base           [T,H] added to the sum (a residual stream, a shared    in
+ *                  expert's output); NULL: 0.  May be `out` itself.
+ *   out            [T,H]                                                  out
+ *   workspace      >= laser_experts_workspace_bytes(...) bytes, 256-byte aligned
+ */
+int laser_experts_down(const void* act, const void* w_down, int32_t T, int32_t H, int32_t F,
+                       int32_t E, const laser_experts_params_t* params,
+                       const int32_t* permutation, const int32_t* expert_offsets,
+                       const int32_t* expert_ids, const float* weights, const void* base, void* out,
+                       void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * A projection that all rows of a batch share, beside it the low-rank adapters that the
+ * batch's requests bring along (a gate whose requests have adapters of their own: fp32
+ * output, which laser_route_from_logits takes; or any other projection of the layer).
+ */
+#define LASER_MAX_RANK 128
+typedef struct laser_adapter_params {
+  uint32_t struct_bytes; /* = sizeof(laser_adapter_params_t)                           */
+  int32_t rank;          /* R, rows of an adapter's inner matrix (smaller ranks: rows  */
+                         /* of zeros); a multiple of 8 (bf16) or 4 (fp32), <= 128      */
+  int32_t adapters;      /* M, adapters in a_down, a_up and scales; may be 0           */
+  int32_t requests;      /* requests in the batch; may be 0                            */
+  int32_t dtype;         /* LASER_DTYPE_* of x, w, a_down and a_up                     */
+  int32_t out_dtype;     /* LASER_DTYPE_* of out: that of the inputs, or fp32          */
+} laser_adapter_params_t;
+
+/* Bytes of device workspace laser_project_adapted needs (0 on bad arguments); enough for
+ * every call with fewer rows as well. */
+size_t laser_project_workspace_bytes(int32_t T, int32_t H, int32_t N,
+                                     const laser_adapter_params_t* params);
+
+/*
+ *   out[t,n] = sum_h x[t,h] w[n,h] + scales[m] sum_r a_up[m,n,r] (sum_h a_down[m,r,h] x[t,h])
+ * where m is the adapter of the request that row t belongs to; the second term is absent
+ * for rows that belong to no request and for requests without an adapter.  All sums, the
+ * inner one among them, are held in fp32; out is rounded once.
+ *   x                [T,H]                                                in
+ *   w                [N,H]                                                in
+ *   a_down           [M,R,H], a_up [M,N,R]                                in
+ *   scales           [M] fp32; NULL: 1                                    in
+ *   request_offsets  [requests+1] int32, ascending: request q has the     in
+ *                    rows request_offsets[q] .. request_offsets[q+1]-1 (maybe none)
+ *   request_adapters [requests] int32: its adapter; outside [0,M): none   in
+ *   out              [T,N]                                                out
+ *   workspace        >= laser_project_workspace_bytes(...) bytes, 256-byte aligned
+ * a_down, a_up, request_offsets and request_adapters may be NULL if there are no adapters
+ * or no requests.  H a multiple of 8 (bf16) or 4 (fp32), matrices 16-byte aligned and
+ * without gaps between rows; N is free.
+ */
+int laser_project_adapted(const void* x, const void* w, int32_t T, int32_t H, int32_t N,
+                          const laser_adapter_params_t* params, const void* a_down,
+                          const void* a_up, const float* scales, const int32_t* request_offsets,
+                          const int32_t* request_adapters, void* out, void* workspace,
+                          size_t workspace_bytes, void* hip_stream);
+
 /* Static, NUL-terminated description of a return code (host pointer). */
 const char* laser_strerror(int code);
 

@@ -23,7 +23,8 @@ TRIM_RANDOM = 1
 EXPORTS = ("laser_workspace_bytes", "laser_route", "laser_route_batched", "laser_route_stats",
            "laser_route_from_logits", "laser_imbalance", "laser_percentiles", "laser_summary_f32",
            "laser_strerror", "laser_status", "laser_static_workspace_bytes", "laser_route_static",
-           "laser_status_static")
+           "laser_status_static", "laser_experts_up", "laser_experts_workspace_bytes", "laser_experts_down",
+           "laser_project_workspace_bytes", "laser_project_adapted")
 # include/laser_bench.h
 BENCH_EXPORTS = ("laser_bench_timer_create", "laser_bench_timer_destroy", "laser_bench_route",
                  "laser_bench_timer_read", "laser_bench_event_overhead", "laser_bench_plain_read")
@@ -49,6 +50,26 @@ class LaserParams(ctypes.Structure):
         ("poll_budget", ctypes.c_uint32),
         ("pipeline_tiles", ctypes.c_uint32),
         ("split_k", ctypes.c_uint32),
+    ]
+
+
+class LaserExpertsParams(ctypes.Structure):
+    _fields_ = [
+        ("struct_bytes", ctypes.c_uint32),
+        ("k", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("first_expert", ctypes.c_int32),
+    ]
+
+
+class LaserAdapterParams(ctypes.Structure):
+    _fields_ = [
+        ("struct_bytes", ctypes.c_uint32),
+        ("rank", ctypes.c_int32),
+        ("adapters", ctypes.c_int32),
+        ("requests", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("out_dtype", ctypes.c_int32),
     ]
 
 
@@ -93,6 +114,17 @@ def _load() -> ctypes.CDLL:
     lib.laser_route_static.restype = ctypes.c_int
     lib.laser_status_static.argtypes = [vp, ctypes.POINTER(ctypes.c_int32)]
     lib.laser_status_static.restype = ctypes.c_int
+    ep, ap = ctypes.POINTER(LaserExpertsParams), ctypes.POINTER(LaserAdapterParams)
+    lib.laser_experts_up.argtypes = [vp, vp, i32, i32, i32, i32, ep, vp, vp, vp, vp]
+    lib.laser_experts_up.restype = ctypes.c_int
+    lib.laser_experts_workspace_bytes.argtypes = [i32, i32, i32, i32, ep]
+    lib.laser_experts_workspace_bytes.restype = sz
+    lib.laser_experts_down.argtypes = [vp, vp, i32, i32, i32, i32, ep, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.laser_experts_down.restype = ctypes.c_int
+    lib.laser_project_workspace_bytes.argtypes = [i32, i32, i32, ap]
+    lib.laser_project_workspace_bytes.restype = sz
+    lib.laser_project_adapted.argtypes = [vp, vp, i32, i32, i32, ap, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.laser_project_adapted.restype = ctypes.c_int
     lib.laser_bench_timer_create.argtypes = [i32, ctypes.POINTER(vp)]
     lib.laser_bench_timer_create.restype = ctypes.c_int
     lib.laser_bench_timer_destroy.argtypes = [vp]
@@ -246,6 +278,48 @@ def laser_status_static(stream=None) -> int:
     return st.value
 
 
+def make_experts_params(k: int, dtype: int = DTYPE_BF16, first_expert: int = 0) -> LaserExpertsParams:
+    return LaserExpertsParams(ctypes.sizeof(LaserExpertsParams), k, dtype, first_expert)
+
+
+def make_adapter_params(rank: int, adapters: int, requests: int, dtype: int = DTYPE_BF16,
+                        out_dtype: int | None = None) -> LaserAdapterParams:
+    return LaserAdapterParams(ctypes.sizeof(LaserAdapterParams), rank, adapters, requests, dtype,
+                              dtype if out_dtype is None else out_dtype)
+
+
+def laser_experts_up(hidden, w_up, T, H, F, E, params, permutation, expert_offsets, act, stream=None) -> None:
+    """Enqueue the experts' first product and activation over the dispatch tables (see laser.h)."""
+    _check(_lib.laser_experts_up(_ptr(hidden), _ptr(w_up), T, H, F, E, ctypes.byref(params),
+                                 _ptr(permutation), _ptr(expert_offsets), _ptr(act), _stream_handle(stream)))
+
+
+def laser_experts_workspace_bytes(T: int, H: int, F: int, E: int, params: LaserExpertsParams) -> int:
+    return int(_lib.laser_experts_workspace_bytes(T, H, F, E, ctypes.byref(params)))
+
+
+def laser_experts_down(act, w_down, T, H, F, E, params, permutation, expert_offsets, expert_ids, weights,
+                       base, out, workspace, stream=None) -> None:
+    """Enqueue the experts' second product, weighted and summed back into token order."""
+    _check(_lib.laser_experts_down(_ptr(act), _ptr(w_down), T, H, F, E, ctypes.byref(params),
+                                   _ptr(permutation), _ptr(expert_offsets), _ptr(expert_ids), _ptr(weights),
+                                   _ptr(base), _ptr(out), _ptr(workspace),
+                                   workspace.numel() * workspace.element_size(), _stream_handle(stream)))
+
+
+def laser_project_workspace_bytes(T: int, H: int, N: int, params: LaserAdapterParams) -> int:
+    return int(_lib.laser_project_workspace_bytes(T, H, N, ctypes.byref(params)))
+
+
+def laser_project_adapted(x, w, T, H, N, params, a_down, a_up, scales, request_offsets, request_adapters,
+                          out, workspace, stream=None) -> None:
+    """Enqueue a shared projection with the adapters of the batch's requests beside it."""
+    _check(_lib.laser_project_adapted(_ptr(x), _ptr(w), T, H, N, ctypes.byref(params), _ptr(a_down), _ptr(a_up),
+                                      _ptr(scales), _ptr(request_offsets), _ptr(request_adapters), _ptr(out),
+                                      _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                      _stream_handle(stream)))
+
+
 class BenchTimer:
     """Event pool of include/laser_bench.h: times the stages of laser_bench_route calls."""
 
@@ -338,3 +412,126 @@ def route_from_logits(logits, params: LaserParams, loads_inout,
     laser_route_from_logits(logits, T, E, params, loads_inout, buffers.expert_ids, buffers.weights,
                             buffers.permutation, buffers.expert_offsets, buffers.workspace, stream)
     return buffers
+
+
+_CODES = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16}
+
+
+def _dtype_code(t: torch.Tensor, name: str) -> int:
+    if t.dtype not in _CODES:
+        raise ValueError(f"{name} must be float32 or bfloat16, not {t.dtype}")
+    return _CODES[t.dtype]
+
+
+def _expect(name: str, t, shape, dtype, device, optional: bool = False) -> None:
+    """Checks one tensor of a wrapped call: its shape, type, device, and that it has no gaps."""
+    if t is None:
+        if optional:
+            return
+        raise ValueError(f"{name} is missing")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not on {device}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
+def _expect_current(device) -> None:
+    """The library launches on the current device, so that is where the tensors have to be."""
+    if device.type != "cuda" or device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors are on {device}: they must be on the current GPU")
+
+
+class ExpertBuffers:
+    """act, out and workspace of experts() for calls of one size, allocated once."""
+
+    def __init__(self, T: int, H: int, F: int, E: int, k: int, dtype: torch.dtype, device="cuda"):
+        if dtype not in _CODES:
+            raise ValueError(f"dtype must be float32 or bfloat16, not {dtype}")
+        nbytes = laser_experts_workspace_bytes(T, H, F, E, make_experts_params(k, _CODES[dtype]))
+        if nbytes == 0:
+            raise LaserError(-2, "laser_experts_workspace_bytes rejected the arguments")
+        self.act = torch.empty((T * k, F), dtype=dtype, device=device)
+        self.out = torch.empty((T, H), dtype=dtype, device=device)
+        self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def experts(hidden, w_up, w_down, routed: RouteBuffers | None, base=None, first_expert: int = 0,
+            buffers: ExpertBuffers | None = None, stream=None) -> ExpertBuffers:
+    """Both products of the experts behind a routing call: laser_experts_up, then laser_experts_down
+    with the call's weights.  w_up [E,2F,H], w_down [E,H,F]; routed None: one expert (E = 1) for every
+    token.  The result is `out` of the returned buffers."""
+    code = _dtype_code(hidden, "hidden")
+    if hidden.dim() != 2 or w_down.dim() != 3:
+        raise ValueError("hidden must have 2 dimensions, w_down 3")
+    (T, H), (E, _, F), dev, dt = hidden.shape, w_down.shape, hidden.device, hidden.dtype
+    k = 1 if routed is None else routed.k
+    _expect("hidden", hidden, (T, H), dt, dev)
+    _expect("w_up", w_up, (E, 2 * F, H), dt, dev)
+    _expect("w_down", w_down, (E, H, F), dt, dev)
+    _expect("base", base, (T, H), dt, dev, optional=True)
+    if routed is not None:
+        _expect("permutation", routed.permutation, (T * k,), torch.int32, dev)
+        _expect("expert_ids", routed.expert_ids, (T, k), torch.int32, dev)
+        _expect("weights", routed.weights, (T, k), torch.float32, dev)
+        total = routed.expert_offsets.numel() - 1
+        _expect("expert_offsets", routed.expert_offsets, (total + 1,), torch.int32, dev)
+        if first_expert < 0 or first_expert + E > total:
+            raise ValueError(f"experts {first_expert} to {first_expert + E - 1} of {total}")
+    if buffers is not None:
+        _expect("buffers.act", buffers.act, (T * k, F), dt, dev)
+        _expect("buffers.out", buffers.out, (T, H), dt, dev)
+    _expect_current(dev)
+    if buffers is None:
+        buffers = ExpertBuffers(T, H, F, E, k, dt, device=dev)
+    params = make_experts_params(k, code, first_expert)
+    tables = (None,) * 4 if routed is None else (routed.permutation, routed.expert_offsets, routed.expert_ids,
+                                                 routed.weights)
+    laser_experts_up(hidden, w_up, T, H, F, E, params, tables[0], tables[1], buffers.act, stream)
+    laser_experts_down(buffers.act, w_down, T, H, F, E, params, *tables, base, buffers.out, buffers.workspace, stream)
+    return buffers
+
+
+class ProjectBuffers:
+    """out and workspace of project_adapted() for calls of one size, allocated once."""
+
+    def __init__(self, T: int, H: int, N: int, params: LaserAdapterParams, device="cuda"):
+        nbytes = laser_project_workspace_bytes(T, H, N, params)
+        if nbytes == 0:
+            raise LaserError(-2, "laser_project_workspace_bytes rejected the arguments")
+        dtype = torch.float32 if params.out_dtype == DTYPE_F32 else torch.bfloat16
+        self.out = torch.empty((T, N), dtype=dtype, device=device)
+        self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def project_adapted(x, w, a_down, a_up, scales, request_offsets, request_adapters, out_dtype=None,
+                    buffers: ProjectBuffers | None = None, stream=None) -> torch.Tensor:
+    """laser_project_adapted with sizes from the tensors: x [T,H], w [N,H], a_down [M,R,H], a_up [M,N,R],
+    scales [M] fp32 or None, request_offsets [requests+1] and request_adapters [requests] int32.
+    out_dtype: that of x (default) or float32.  Returns out [T,N]."""
+    code = _dtype_code(x, "x")
+    if x.dim() != 2 or w.dim() != 2 or a_down.dim() != 3 or request_adapters.dim() != 1:
+        raise ValueError("x and w must have 2 dimensions, a_down 3, request_adapters 1")
+    (T, H), N, (M, R), n, dev, dt = x.shape, w.shape[0], a_down.shape[:2], request_adapters.numel(), x.device, x.dtype
+    out_dtype = dt if out_dtype is None else out_dtype
+    if out_dtype not in (dt, torch.float32):
+        raise ValueError(f"out_dtype must be {dt} or float32, not {out_dtype}")
+    _expect("x", x, (T, H), dt, dev)
+    _expect("w", w, (N, H), dt, dev)
+    _expect("a_down", a_down, (M, R, H), dt, dev)
+    _expect("a_up", a_up, (M, N, R), dt, dev)
+    _expect("scales", scales, (M,), torch.float32, dev, optional=True)
+    _expect("request_offsets", request_offsets, (n + 1,), torch.int32, dev)
+    _expect("request_adapters", request_adapters, (n,), torch.int32, dev)
+    if buffers is not None:
+        _expect("buffers.out", buffers.out, (T, N), out_dtype, dev)
+    _expect_current(dev)
+    params = make_adapter_params(R, M, n, code, _CODES[out_dtype])
+    if buffers is None:
+        buffers = ProjectBuffers(T, H, N, params, device=dev)
+    laser_project_adapted(x, w, T, H, N, params, a_down, a_up, scales, request_offsets, request_adapters,
+                          buffers.out, buffers.workspace, stream)
+    return buffers.out

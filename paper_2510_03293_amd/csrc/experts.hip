@@ -1,0 +1,280 @@
+// The experts of a layer over the routing tables: laser_experts_up and laser_experts_down.
+#include "../../include/laser.h"
+#include "grouped.h"
+
+namespace laser {
+
+struct ExpertArgs {
+  const unsigned char* x;    // rows of the token operand
+  const unsigned char* w;    // [E, rows of an expert, K]
+  const int32_t* permutation;  // NULL: one group, position = slot = row
+  const int32_t* offsets;      // [E + 1] of the call's experts
+  const float* weights;
+  void* out;
+  int slots;   // T * k
+  int k;
+  int E;
+  int K;       // bytes of a row of either operand
+  int F;       // experts_up: columns of act
+  int H;       // experts_down: columns of out
+};
+
+// Which expert tile `mt` of BM rows belongs to: per lane one expert, tiles counted in order.
+struct ExpertTiles {
+  int lo, cnt, before, total;  // this lane's expert: first position, positions, tiles of earlier experts
+  __device__ void init(const ExpertArgs& a, int lane, int BM) {
+    if (a.offsets == nullptr) {
+      lo = 0;
+      cnt = lane == 0 ? a.slots : 0;
+    } else {
+      // (offsets are the caller's: whatever they hold, positions stay inside the tables)
+      lo = lane < a.E ? min(max(a.offsets[lane], 0), a.slots) : 0;
+      cnt = lane < a.E ? max(min(a.offsets[lane + 1], a.slots) - lo, 0) : 0;
+    }
+    const int tiles = (cnt + BM - 1) / BM;
+    int sum = tiles;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int up = __shfl_up(sum, d);
+      sum += lane >= d ? up : 0;
+    }
+    before = sum - tiles;
+    total = __builtin_amdgcn_readlane(sum, 63);
+  }
+  // expert, first position and rows of tile mt < total
+  __device__ void find(int mt, int BM, int& e, int& p0, int& rows) const {
+    e = 63 - __builtin_clzll(__ballot(before <= mt && cnt > 0));
+    const int in = (mt - __builtin_amdgcn_readlane(before, e)) * BM;
+    p0 = __builtin_amdgcn_readlane(lo, e) + in;
+    rows = min(__builtin_amdgcn_readlane(cnt, e) - in, BM);
+  }
+};
+
+template <bool F32>
+__device__ __forceinline__ float silu(float g) {
+  // g / (1 + exp(-g)); a large negative g divides by infinity and gives -0
+  if constexpr (F32) return g / (1.0f + expf(-g));
+  return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.44269504f));
+}
+
+template <bool F32, bool UP, class TL>
+__global__ __launch_bounds__(TL::kThreads) void experts_kernel(ExpertArgs a) {
+  extern __shared__ __align__(1024) unsigned char ring[];
+  const unsigned lds = (unsigned)(size_t)(lds_bytes)ring;
+  constexpr int BM = TL::BM, BN = TL::BN, NB = TL::NB, MB = TL::MB;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  ExpertTiles tiles;
+  tiles.init(a, lane, BM);
+  constexpr int kCols = UP ? BN / 2 : BN;  // output columns of a tile
+  const int cols = UP ? a.F : a.H;
+  const int nt = (cols + kCols - 1) / kCols;
+  const int total = tiles.total * nt;
+  const int wm = wave % TL::WM, wn = wave / TL::WM;
+  constexpr int kWaveCols = kCols / TL::WN;
+  for (int v = blockIdx.x; v < total; v += gridDim.x) {
+    const int id = xcd_run(v, total);
+    constexpr int kGroup = 4;  // tiles of rows that walk the columns together
+    const int g = id / (kGroup * nt), gm = min(kGroup, tiles.total - g * kGroup), in = id - g * kGroup * nt;
+    const int mt = g * kGroup + in % gm, c0 = in / gm * kCols;
+    int e, p0, rows;
+    tiles.find(mt, BM, e, p0, rows);
+
+    const unsigned char* from[TL::kLoads];
+    const int piece = TL::piece(wave, lane) * 16;
+#pragma unroll
+    for (int i = 0; i < TL::kLoads; ++i) {
+      const int r = TL::row(wave, lane, i);
+      if (r < BM) {
+        const int p = p0 + min(r, rows - 1);
+        int row = p;
+        if (UP && a.permutation != nullptr) row = min(max(a.permutation[p], 0), a.slots - 1) / a.k;
+        from[i] = a.x + (size_t)row * a.K + piece;
+      } else {
+        int n = r - BM, row;
+        if constexpr (UP) {  // a wavefront's rows: first of the gate matrix, then the same of the up matrix
+          const int half = n % (2 * kWaveCols) / kWaveCols;
+          row = half * a.F + min(c0 + n / (2 * kWaveCols) * kWaveCols + n % kWaveCols, a.F - 1);
+        } else {
+          row = min(c0 + n, a.H - 1);
+        }
+        from[i] = a.w + ((size_t)e * (UP ? 2 * a.F : a.H) + row) * a.K + piece;
+      }
+    }
+    mma_f32x4 acc[NB][MB];
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+      for (int m = 0; m < MB; ++m) acc[n][m] = mma_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    TL::run(from, a.K, lds, wave, lane, acc);
+
+#pragma unroll
+    for (int m = 0; m < MB; ++m) {
+      const int r = wm * (BM / TL::WM) + m * 16 + (lane & 15);
+      if (r >= rows) continue;
+      const int p = p0 + r;
+      if constexpr (UP) {
+#pragma unroll
+        for (int n = 0; n < NB / 2; ++n) {
+          const int f = c0 + wn * kWaveCols + n * 16 + 4 * (lane >> 4);
+          mma_f32x4 y;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) y[i] = silu<F32>(acc[n][m][i]) * acc[NB / 2 + n][m][i];
+          if (f < a.F) store4<F32>(a.out, (size_t)p * a.F + f, y);
+        }
+      } else {
+        const int slot = a.permutation != nullptr ? min(max(a.permutation[p], 0), a.slots - 1) : p;
+        const float weight = a.weights != nullptr ? a.weights[slot] : 1.0f;
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+          const int h = c0 + wn * kWaveCols + n * 16 + 4 * (lane >> 4);
+          if (h < a.H) store4<true>(a.out, (size_t)slot * a.H + h, acc[n][m] * weight);
+        }
+      }
+    }
+  }
+}
+
+// out[t,:] = base[t,:] + the products of the token's slots that the call's experts hold, in
+// slot order.  One thread per four columns.
+template <bool F32>
+__global__ __launch_bounds__(256) void experts_combine_kernel(const float* z, const int32_t* ids, const void* base,
+                                                              void* out, int T, int H, int k, int first, int E) {
+  const int quads = H >> 2;
+  const size_t all = (size_t)T * quads;
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (size_t)gridDim.x * 256) {
+    const size_t t = i / quads;
+    const int h = (int)(i - t * quads) * 4;
+    mma_f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (base != nullptr) y = load4<F32>(base, t * H + h);
+    for (int j = 0; j < k; ++j) {
+      const size_t slot = t * k + j;
+      if (ids == nullptr || (unsigned)(ids[slot] - first) < (unsigned)E)
+        y += *reinterpret_cast<const mma_f32x4*>(z + slot * H + h);
+    }
+    store4<F32>(out, t * H + h, y);
+  }
+}
+
+constexpr int kGridMost = 1 << 20;
+
+template <bool F32, bool UP, class TL>
+static hipError_t launch_experts(const ExpertArgs& a, hipStream_t s) {
+  static LdsAttr attr;
+  const void* fn = reinterpret_cast<const void*>(&experts_kernel<F32, UP, TL>);
+  hipError_t err = allow_dynamic_lds(fn, TL::kLdsBytes, attr);
+  if (err != hipSuccess) return err;
+  // (every expert with rows has at most one tile that is not full, and every tile a row)
+  const long long mt = min((long long)a.slots, (long long)a.slots / TL::BM + min(a.E, a.slots));
+  const int cols = UP ? TL::BN / 2 : TL::BN;
+  const long long grid = mt * (((UP ? a.F : a.H) + cols - 1) / cols);
+  hipLaunchKernelGGL((experts_kernel<F32, UP, TL>), dim3((unsigned)min(grid, (long long)kGridMost)),
+                     dim3(TL::kThreads), TL::kLdsBytes, s, a);
+  return hipGetLastError();
+}
+
+static int check_experts(int32_t T, int32_t H, int32_t F, int32_t E, const laser_experts_params_t* p) {
+  if (!p) return LASER_E_NULL;
+  if (p->struct_bytes != sizeof(laser_experts_params_t)) return LASER_E_STRUCT;
+  if (T < 0 || H < 1 || F < 1 || E < 1 || p->k < 1 || p->first_expert < 0) return LASER_E_RANGE;
+  if ((int64_t)T * p->k > 0x7fffffffLL || F > (1 << 28) || H > (1 << 28)) return LASER_E_RANGE;
+  if (p->dtype != LASER_DTYPE_F32 && p->dtype != LASER_DTYPE_BF16) return LASER_E_RANGE;
+  if (p->k > LASER_MAX_K || E > LASER_MAX_E - p->first_expert) return LASER_E_UNSUPPORTED;
+  const int whole = p->dtype == LASER_DTYPE_F32 ? 4 : 8;
+  if (H % whole != 0 || F % whole != 0) return LASER_E_ALIGN;
+  return LASER_OK;
+}
+
+static bool misaligned(const void* p) { return ((uintptr_t)p & 15) != 0; }
+
+// Without tables: one expert that takes every token once.
+static int check_tables(const int32_t* permutation, const int32_t* offsets, int32_t E,
+                        const laser_experts_params_t* p) {
+  if (permutation && offsets) return LASER_OK;
+  if (permutation || offsets) return LASER_E_NULL;
+  return E == 1 && p->k == 1 && p->first_expert == 0 ? LASER_OK : LASER_E_NULL;
+}
+
+}  // namespace laser
+
+using namespace laser;
+
+extern "C" int laser_experts_up(const void* hidden, const void* w_up, int32_t T, int32_t H, int32_t F, int32_t E,
+                                const laser_experts_params_t* params, const int32_t* permutation,
+                                const int32_t* expert_offsets, void* act, void* hip_stream) {
+  int rc = check_experts(T, H, F, E, params);
+  if (rc != LASER_OK) return rc;
+  if (T == 0) return LASER_OK;
+  if (!hidden || !w_up || !act) return LASER_E_NULL;
+  rc = check_tables(permutation, expert_offsets, E, params);
+  if (rc != LASER_OK) return rc;
+  if (misaligned(hidden) || misaligned(w_up) || misaligned(act)) return LASER_E_ALIGN;
+  const bool f32 = params->dtype == LASER_DTYPE_F32;
+  ExpertArgs a = {};
+  a.x = static_cast<const unsigned char*>(hidden);
+  a.w = static_cast<const unsigned char*>(w_up);
+  a.permutation = permutation;
+  a.offsets = expert_offsets ? expert_offsets + params->first_expert : nullptr;
+  a.out = act;
+  a.slots = T * params->k;
+  a.k = params->k;
+  a.E = E;
+  a.K = H * (f32 ? 4 : 2);
+  a.F = F;
+  a.H = H;
+  clear_stale_error();
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  const hipError_t err = f32 ? launch_experts<true, true, Tile<true, 64, 128, 1, 4, 3>>(a, s)
+                             : launch_experts<false, true, Tile<false, 64, 128, 1, 4, 3>>(a, s);
+  return err == hipSuccess ? LASER_OK : LASER_E_LAUNCH;
+}
+
+extern "C" size_t laser_experts_workspace_bytes(int32_t T, int32_t H, int32_t F, int32_t E,
+                                                const laser_experts_params_t* params) {
+  if (check_experts(T, H, F, E, params) != LASER_OK) return 0;
+  return ((size_t)T * params->k * H * 4 + 256) & ~(size_t)255;
+}
+
+extern "C" int laser_experts_down(const void* act, const void* w_down, int32_t T, int32_t H, int32_t F, int32_t E,
+                                  const laser_experts_params_t* params, const int32_t* permutation,
+                                  const int32_t* expert_offsets, const int32_t* expert_ids, const float* weights,
+                                  const void* base, void* out, void* workspace, size_t workspace_bytes,
+                                  void* hip_stream) {
+  int rc = check_experts(T, H, F, E, params);
+  if (rc != LASER_OK) return rc;
+  if (T == 0) return LASER_OK;
+  if (!act || !w_down || !out || !workspace) return LASER_E_NULL;
+  rc = check_tables(permutation, expert_offsets, E, params);
+  if (rc != LASER_OK) return rc;
+  if (misaligned(act) || misaligned(w_down) || misaligned(out) || misaligned(base)) return LASER_E_ALIGN;
+  if ((uintptr_t)workspace & 255) return LASER_E_ALIGN;
+  if (workspace_bytes < laser_experts_workspace_bytes(T, H, F, E, params)) return LASER_E_WORKSPACE;
+  const bool f32 = params->dtype == LASER_DTYPE_F32;
+  ExpertArgs a = {};
+  a.x = static_cast<const unsigned char*>(act);
+  a.w = static_cast<const unsigned char*>(w_down);
+  a.permutation = permutation;
+  a.offsets = expert_offsets ? expert_offsets + params->first_expert : nullptr;
+  a.weights = weights;
+  a.out = workspace;
+  a.slots = T * params->k;
+  a.k = params->k;
+  a.E = E;
+  a.K = F * (f32 ? 4 : 2);
+  a.F = F;
+  a.H = H;
+  clear_stale_error();
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  const hipError_t err = f32 ? launch_experts<true, false, Tile<true, 64, 128, 1, 4, 3>>(a, s)
+                             : launch_experts<false, false, Tile<false, 64, 128, 1, 4, 3>>(a, s);
+  if (err != hipSuccess) return LASER_E_LAUNCH;
+  const size_t quads = (size_t)T * (H / 4);
+  const unsigned grid = (unsigned)min((quads + 255) / 256, (size_t)1 << 16);
+  const float* z = static_cast<const float*>(workspace);
+  if (f32)
+    hipLaunchKernelGGL((experts_combine_kernel<true>), dim3(grid), dim3(256), 0, s, z, expert_ids, base, out, T, H,
+                       params->k, params->first_expert, E);
+  else
+    hipLaunchKernelGGL((experts_combine_kernel<false>), dim3(grid), dim3(256), 0, s, z, expert_ids, base, out, T, H,
+                       params->k, params->first_expert, E);
+  return hipGetLastError() == hipSuccess ? LASER_OK : LASER_E_LAUNCH;
+}

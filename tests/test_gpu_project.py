@@ -1,0 +1,182 @@
+"""A shared projection with the adapters of the batch's requests beside it against its
+definition in 64 bits."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2510_03293_amd import binding as B
+from tests import products as P
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = B.DTYPE_F32, B.DTYPE_BF16
+
+# T, H, N, R, M, request lengths (the rest of the rows belongs to nobody)
+SHAPES = [
+    (1, 8, 1, 8, 1, [1]),
+    (1, 2048, 64, 16, 4, [1]),
+    (5, 72, 33, 8, 3, [1, 1, 1, 1, 1]),
+    (16, 136, 8, 24, 2, [3, 0, 13]),
+    (64, 2048, 64, 16, 32, [1] * 64),
+    (65, 512, 61, 64, 5, [40, 20]),                 # rows behind the last request
+    (100, 328, 200, 40, 3, [1, 1, 30, 0, 0, 68]),
+    (300, 256, 64, 128, 2, [299, 1]),
+    (130, 1024, 130, 16, 8, [7] * 18),
+    (700, 264, 520, 32, 6, [1, 255, 2, 64, 63, 300]),
+    (1500, 520, 64, 16, 4, [500, 499, 501]),
+    (2100, 136, 264, 64, 3, [2100]),
+    (40, 64, 16, 8, 1, []),                         # no requests
+]
+
+
+def _inputs(T, H, N, R, M, lengths, dtype, seed=0):
+    rng = np.random.default_rng(2000 + seed)
+    cuts = np.concatenate([[0], np.cumsum(lengths)]).astype(np.int32)
+    which = rng.integers(-1, M, len(lengths)).astype(np.int32)
+    return dict(x=P.rounded(rng, (T, H), 1.0, dtype), w=P.rounded(rng, (N, H), 0.05, dtype),
+                a_down=P.rounded(rng, (M, R, H), 1 / np.sqrt(H), dtype), a_up=P.rounded(rng, (M, N, R), 0.2, dtype),
+                scales=(rng.random(M) * 2).astype(np.float32), cuts=cuts, which=which)
+
+
+def _check(i, out_dtype, dtype, label):
+    out = P.run_project(**i, out_dtype=out_dtype, dtype=dtype)
+    want, tol = P.project_reference(**i, out_dtype=out_dtype, dtype=dtype)
+    P.assert_within(P.f64(out), want, tol, label)
+    return out
+
+
+@pytest.mark.parametrize("dtype,out_dtype", [(BF16, F32), (BF16, BF16), (F32, F32)])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "T%d_H%d_N%d_R%d_M%d" % s[:5])
+def test_project(shape, dtype, out_dtype):
+    _check(_inputs(*shape, dtype), out_dtype, dtype, str(shape))
+
+
+@pytest.mark.parametrize("T,H,N", [(3, 64, 8), (200, 256, 64), (300, 136, 200)])
+def test_without_adapters_scales_or_known_ones(T, H, N):
+    """No adapter tensors at all; requests that name adapters that are not there; scales of 1."""
+    i = _inputs(T, H, N, 16, 3, [T // 2, T - T // 2], BF16, seed=1)
+    bare = dict(i, a_down=None, a_up=None, scales=None, cuts=None, which=np.zeros(0, np.int32))
+    plain = P.run_project(**bare, out_dtype=F32, dtype=BF16)
+    want, tol = P.product_bound(P.f64(i["x"]), P.f64(i["w"]), BF16)
+    P.assert_within(P.f64(plain), want, tol + P.U * np.abs(want), "bare")
+    named = dict(i, which=np.array([3, -2 ** 31], dtype=np.int32))
+    assert torch.equal(P.run_project(**named, out_dtype=F32, dtype=BF16), plain)
+    _check(dict(i, scales=None, which=np.array([2, 0], dtype=np.int32)), F32, BF16, "no scales")
+
+
+def test_rows_before_the_first_request():
+    i = _inputs(90, 136, 64, 8, 4, [10, 0, 30], BF16, seed=2)
+    i["cuts"] = i["cuts"] + np.int32(17)
+    i["which"] = np.array([1, 2, 3], np.int32)
+    out = _check(i, F32, BF16, "shifted")
+    none = P.run_project(**dict(i, which=np.full(3, -1, np.int32)), out_dtype=F32, dtype=BF16)
+    assert torch.equal(out[:17], none[:17]) and torch.equal(out[57:], none[57:])
+    assert not torch.equal(out[17:57], none[17:57])
+
+
+@pytest.mark.parametrize("T,H,N", [(20, 72, 64), (400, 200, 96)])
+def test_what_does_not_belong_to_a_row_does_not_reach_it(T, H, N):
+    """Infinities and NaN in other rows, in adapters of other requests and in unused ones."""
+    half = T // 2
+    i = _inputs(T, H, N, 16, 3, [half, T - half], BF16, seed=4)
+    i["which"] = np.array([0, 1], np.int32)
+    clean = P.run_project(**i, out_dtype=F32, dtype=BF16)
+    bad = {n: (v.clone() if torch.is_tensor(v) else v.copy()) for n, v in i.items()}
+    bad["a_down"][1:] = float("nan")
+    bad["a_up"][1:] = float("inf")
+    bad["scales"][1:] = np.inf
+    bad["x"][half - 1] = float("nan")
+    out = P.run_project(**bad, out_dtype=F32, dtype=BF16)
+    assert torch.equal(out[:half - 1], clean[:half - 1])
+    assert torch.isnan(out[half - 1]).all()
+    bare = P.run_project(**dict(bad, which=np.array([0, -1], np.int32)), out_dtype=F32, dtype=BF16)
+    assert torch.isfinite(bare[half:]).all()
+
+
+def test_request_tables_out_of_range_stay_inside_the_arrays():
+    i = _inputs(120, 136, 64, 16, 3, [40, 40, 40], BF16, seed=5)
+    for cuts, which in (([-7, 2 ** 31 - 1, 5, 90], [0, 1, 2]), ([120, 80, 40, 0], [2, 1, 0]),
+                        ([-2 ** 31, -1, 60, 2 ** 31 - 1], [1, 2 ** 31 - 1, 0])):
+        out = P.run_project(**dict(i, cuts=np.array(cuts, np.int32), which=np.array(which, np.int32)), out_dtype=F32,
+                            dtype=BF16)
+        assert torch.isfinite(out).all()
+
+
+def test_rows_beyond_four_gigabytes():
+    T, H, N = 300_000, 8192, 8
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    x = torch.empty(T, H, dtype=torch.bfloat16, device="cuda").normal_(0, 1, generator=g)
+    rng = np.random.default_rng(6)
+    i = _inputs(8, H, N, 8, 2, [4, 4], BF16, seed=6)
+    params = B.make_adapter_params(8, 2, 2, out_dtype=F32)
+    ws = torch.empty(B.laser_project_workspace_bytes(T, H, N, params), dtype=torch.uint8, device="cuda")
+    out = torch.empty(T, N, dtype=torch.float32, device="cuda")
+    cuts = torch.tensor([0, T - 5, T], dtype=torch.int32, device="cuda")
+    which = torch.tensor([1, 0], dtype=torch.int32, device="cuda")
+    B.laser_project_adapted(x, i["w"].cuda(), T, H, N, params, i["a_down"].cuda(), i["a_up"].cuda(),
+                            torch.from_numpy(i["scales"]).cuda(), cuts, which, out, ws)
+    some = np.array([0, 70_000, 262_143, 262_144, T - 6, T - 5, T - 1])
+    rows = x[torch.from_numpy(some).cuda()].cpu()
+    want, tol = P.project_reference(rows, i["w"], i["a_down"], i["a_up"], i["scales"], [0, 5, 7], [1, 0], F32, BF16)
+    P.assert_within(P.f64(out[torch.from_numpy(some).cuda()]), want, tol, "far rows")
+
+
+def test_the_gate_of_a_batch_of_adapted_requests():
+    """Adapted logits routed by laser_route_from_logits, then the experts: the whole layer."""
+    T, H, E, k, F, M = 200, 256, 16, 4, 72, 3
+    i = _inputs(T, H, E, 16, M, [50, 1, 149], BF16, seed=8)
+    i["which"] = np.array([0, 2, -1], np.int32)
+    dev = {n: (v if torch.is_tensor(v) else torch.from_numpy(v)).cuda() for n, v in i.items()}
+    logits = B.project_adapted(dev["x"], dev["w"], dev["a_down"], dev["a_up"], dev["scales"], dev["cuts"],
+                               dev["which"], out_dtype=torch.float32)
+    want, tol = P.project_reference(**i, out_dtype=F32, dtype=BF16)
+    P.assert_within(P.f64(logits), want, tol, "logits")
+    params = B.make_params(k, 6, 0.4, 0.8)
+    routed = B.route_from_logits(logits, params, torch.zeros(E, dtype=torch.int32, device="cuda"))
+    import oracle
+    ref = oracle.route(logits.cpu().numpy(), k, 6, 0.4, 0.8, np.zeros(E, np.int32))
+    assert np.array_equal(routed.expert_ids.cpu().numpy(), ref["expert_ids"])
+    rng = np.random.default_rng(9)
+    w_up, w_down = P.rounded(rng, (E, 2 * F, H), 0.1, BF16).cuda(), P.rounded(rng, (E, H, F), 0.1, BF16).cuda()
+    layer = B.experts(dev["x"], w_up, w_down, routed, base=dev["x"])
+    perm, offs, ids = (t.cpu().numpy() for t in (routed.permutation, routed.expert_offsets, routed.expert_ids))
+    want, tol = P.down_reference(layer.act, w_down, perm, offs, ids, routed.weights.cpu().numpy(), dev["x"], k, 0, T,
+                                 BF16)
+    P.assert_within(P.f64(layer.out), want, tol, "layer")
+
+
+def test_replayed_from_a_graph_and_on_another_stream():
+    i = _inputs(70, 512, 64, 16, 8, [1] * 70, BF16, seed=10)
+    dev = {n: (v if torch.is_tensor(v) else torch.from_numpy(v)).cuda() for n, v in i.items()}
+    buf = B.ProjectBuffers(70, 512, 64, B.make_adapter_params(16, 8, 70, out_dtype=F32))
+
+    def step(stream=None):
+        return B.project_adapted(dev["x"], dev["w"], dev["a_down"], dev["a_up"], dev["scales"], dev["cuts"],
+                                 dev["which"], out_dtype=torch.float32, buffers=buf, stream=stream)
+
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    inputs = [torch.empty_like(dev["x"]).normal_(0, 1, generator=g) for _ in range(3)]
+    want = []
+    for x in inputs:
+        dev["x"].copy_(x)
+        want.append(step().clone())
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for x, w in zip(inputs + inputs, want + want):
+        dev["x"].copy_(x)
+        buf.out.fill_(777.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(buf.out, w)
+    dev["x"].copy_(inputs[1])
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    step(side)
+    side.synchronize()
+    assert torch.equal(buf.out, want[1])
