@@ -57,37 +57,55 @@ __device__ __forceinline__ float silu(float g) {
   return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.44269504f));
 }
 
+// A workgroup computes tiles v, v + grid, ...; what the next one needs first is fetched while
+// the one before is computed: its rows' entries of the permutation before run(), its first
+// steps before the results are written.
 template <bool F32, bool UP, class TL>
 __global__ __launch_bounds__(TL::kThreads) void experts_kernel(ExpertArgs a) {
   extern __shared__ __align__(1024) unsigned char ring[];
-  const unsigned lds = (unsigned)(size_t)(lds_bytes)ring;
   constexpr int BM = TL::BM, BN = TL::BN, NB = TL::NB, MB = TL::MB;
+  static_assert(BM <= TL::kThreads, "one thread per row of the tile");
+  // behind the ring: per row of the tile its token (UP) or its slot and weight
+  int* const row_of = reinterpret_cast<int*>(ring + TL::kLdsBytes);
+  float* const weight_of = reinterpret_cast<float*>(row_of + 2 * BM);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   ExpertTiles tiles;
   tiles.init(a, lane, BM);
   constexpr int kCols = UP ? BN / 2 : BN;  // output columns of a tile
+  constexpr int kWaveCols = kCols / TL::WN;
   const int cols = UP ? a.F : a.H;
   const int nt = (cols + kCols - 1) / kCols;
   const int total = tiles.total * nt;
-  const int wm = wave % TL::WM, wn = wave / TL::WM;
-  constexpr int kWaveCols = kCols / TL::WN;
-  for (int v = blockIdx.x; v < total; v += gridDim.x) {
-    const int id = xcd_run(v, total);
-    constexpr int kGroup = 4;  // tiles of rows that walk the columns together
-    const int g = id / (kGroup * nt), gm = min(kGroup, tiles.total - g * kGroup), in = id - g * kGroup * nt;
-    const int mt = g * kGroup + in % gm, c0 = in / gm * kCols;
-    int e, p0, rows;
-    tiles.find(mt, BM, e, p0, rows);
+  const int wn = wave / TL::WM;
+  const unsigned lds = (unsigned)(size_t)(lds_bytes)ring;
+  const TL tile(a.K, lds, wave, lane);
 
-    const unsigned char* from[TL::kLoads];
+  int e, p0, rows, c0;
+  auto find = [&](int v) {
+    const int id = xcd_run(v, total);
+    constexpr int kGroup = 8;  // tiles of rows that walk the columns together
+    const int g = id / (kGroup * nt), gm = min(kGroup, tiles.total - g * kGroup), in = id - g * kGroup * nt;
+    c0 = in / gm * kCols;
+    tiles.find(g * kGroup + in % gm, BM, e, p0, rows);
+  };
+  // this thread's row of the tile: its slot (rows past the end repeat the last one)
+  auto slot_of = [&]() {
+    const int p = p0 + min((int)threadIdx.x, rows - 1);
+    return a.permutation != nullptr && threadIdx.x < BM ? a.permutation[p] : p;
+  };
+  auto put_row = [&](int slot, int buf) {
+    slot = min(max(slot, 0), a.slots - 1);
+    if (threadIdx.x < BM) row_of[buf * BM + threadIdx.x] = UP ? slot / a.k : slot;
+    return slot;
+  };
+  const unsigned char* from[TL::kLoads];
+  auto begin = [&](int buf, int lane) {
     const int piece = TL::piece(wave, lane) * 16;
 #pragma unroll
     for (int i = 0; i < TL::kLoads; ++i) {
       const int r = TL::row(wave, lane, i);
       if (r < BM) {
-        const int p = p0 + min(r, rows - 1);
-        int row = p;
-        if (UP && a.permutation != nullptr) row = min(max(a.permutation[p], 0), a.slots - 1) / a.k;
+        const int row = UP ? row_of[buf * BM + r] : p0 + min(r, rows - 1);
         from[i] = a.x + (size_t)row * a.K + piece;
       } else {
         int n = r - BM, row;
@@ -100,37 +118,75 @@ __global__ __launch_bounds__(TL::kThreads) void experts_kernel(ExpertArgs a) {
         from[i] = a.w + ((size_t)e * (UP ? 2 * a.F : a.H) + row) * a.K + piece;
       }
     }
+  };
+
+  int v = blockIdx.x, buf = 0;
+  if (v >= total) return;
+  find(v);
+  int slot = put_row(slot_of(), buf);
+  lds_barrier();
+  begin(buf, lane);
+  tile.start(from);
+  for (;;) {
+    const int now_p0 = p0, now_rows = rows, now_c0 = c0;
+    float weight = 1.0f;
+    if (!UP && a.weights != nullptr && threadIdx.x < BM) weight = a.weights[slot];
+    v += gridDim.x;
+    if (v < total) {
+      find(v);
+      slot = slot_of();
+    }
     mma_f32x4 acc[NB][MB];
 #pragma unroll
     for (int n = 0; n < NB; ++n)
 #pragma unroll
       for (int m = 0; m < MB; ++m) acc[n][m] = mma_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    TL::run(from, a.K, lds, wave, lane, acc);
+    tile.run(from, TL::blocks_of(wave, now_rows), acc);
 
-#pragma unroll
-    for (int m = 0; m < MB; ++m) {
-      const int r = wm * (BM / TL::WM) + m * 16 + (lane & 15);
-      if (r >= rows) continue;
-      const int p = p0 + r;
-      if constexpr (UP) {
-#pragma unroll
-        for (int n = 0; n < NB / 2; ++n) {
-          const int f = c0 + wn * kWaveCols + n * 16 + 4 * (lane >> 4);
-          mma_f32x4 y;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) y[i] = silu<F32>(acc[n][m][i]) * acc[NB / 2 + n][m][i];
-          if (f < a.F) store4<F32>(a.out, (size_t)p * a.F + f, y);
-        }
-      } else {
-        const int slot = a.permutation != nullptr ? min(max(a.permutation[p], 0), a.slots - 1) : p;
-        const float weight = a.weights != nullptr ? a.weights[slot] : 1.0f;
-#pragma unroll
-        for (int n = 0; n < NB; ++n) {
-          const int h = c0 + wn * kWaveCols + n * 16 + 4 * (lane >> 4);
-          if (h < a.H) store4<true>(a.out, (size_t)slot * a.H + h, acc[n][m] * weight);
-        }
-      }
+    if (!UP && threadIdx.x < BM) weight_of[threadIdx.x] = weight;
+    if (v < total) slot = put_row(slot, buf ^ 1);
+    lds_barrier();
+    // (what follows depends on the lane alone: kept from moving out of the loop, where it would
+    // occupy the registers that the products need)
+    int l = lane;
+    asm volatile("" : "+v"(l));
+    if (v < total) {
+      begin(buf ^ 1, l);
+      if (TL::ST == 2) tile.start_first(from);
     }
+    const unsigned staging = lds + (TL::ST == 2 ? TL::kStage : 0);
+    if constexpr (UP) {
+      store_tile<F32, TL, NB / 2>(
+          staging, wave, l,
+          [&](int n, int m) {
+            mma_f32x4 y;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] = silu<F32>(acc[n][m][i]) * acc[NB / 2 + n][m][i];
+            return y;
+          },
+          [&](int r, int c) -> void* {
+            const int f = now_c0 + wn * kWaveCols + c;
+            return r < now_rows && f < a.F ? static_cast<char*>(a.out) + ((size_t)(now_p0 + r) * a.F + f) * (F32 ? 4 : 2)
+                                           : nullptr;
+          });
+    } else {
+      float by[MB];
+#pragma unroll
+      for (int m = 0; m < MB; ++m) by[m] = weight_of[TL::block_row(wave, m) + (l & 15)];
+      store_tile<true, TL, NB>(
+          staging, wave, l, [&](int n, int m) { return acc[n][m] * by[m]; },
+          [&](int r, int c) -> void* {
+            const int h = now_c0 + wn * kWaveCols + c;
+            return r < now_rows && h < a.H ? static_cast<float*>(a.out) + (size_t)row_of[buf * BM + r] * a.H + h : nullptr;
+          });
+    }
+    if (v >= total) break;
+    lds_barrier();  // (everybody's results have left the ring)
+    if (TL::ST == 2)
+      tile.start_second(from);
+    else
+      tile.start(from);
+    buf ^= 1;
   }
 }
 
@@ -156,19 +212,22 @@ __global__ __launch_bounds__(256) void experts_combine_kernel(const float* z, co
 }
 
 constexpr int kGridMost = 1 << 20;
+constexpr int kLdsOfCu = 160 << 10;
 
 template <bool F32, bool UP, class TL>
 static hipError_t launch_experts(const ExpertArgs& a, hipStream_t s) {
   static LdsAttr attr;
+  constexpr int kLds = TL::kLdsBytes + TL::BM * 12;  // the ring, and the table of the tile's rows
   const void* fn = reinterpret_cast<const void*>(&experts_kernel<F32, UP, TL>);
-  hipError_t err = allow_dynamic_lds(fn, TL::kLdsBytes, attr);
+  hipError_t err = allow_dynamic_lds(fn, kLds, attr);
   if (err != hipSuccess) return err;
   // (every expert with rows has at most one tile that is not full, and every tile a row)
   const long long mt = min((long long)a.slots, (long long)a.slots / TL::BM + min(a.E, a.slots));
   const int cols = UP ? TL::BN / 2 : TL::BN;
   const long long grid = mt * (((UP ? a.F : a.H) + cols - 1) / cols);
-  hipLaunchKernelGGL((experts_kernel<F32, UP, TL>), dim3((unsigned)min(grid, (long long)kGridMost)),
-                     dim3(TL::kThreads), TL::kLdsBytes, s, a);
+  const long long most = kLds > kLdsOfCu / 2 ? compute_units() : kGridMost;
+  hipLaunchKernelGGL((experts_kernel<F32, UP, TL>), dim3((unsigned)min(grid, most)),
+                     dim3(TL::kThreads), kLds, s, a);
   return hipGetLastError();
 }
 
@@ -224,6 +283,7 @@ extern "C" int laser_experts_up(const void* hidden, const void* w_up, int32_t T,
   clear_stale_error();
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   const hipError_t err = f32 ? launch_experts<true, true, Tile<true, 64, 128, 1, 4, 3>>(a, s)
+                         : a.slots >= 128 * a.E ? launch_experts<false, true, Tile<false, 256, 256, 2, 4, 2>>(a, s)
                              : launch_experts<false, true, Tile<false, 64, 128, 1, 4, 3>>(a, s);
   return err == hipSuccess ? LASER_OK : LASER_E_LAUNCH;
 }
@@ -265,6 +325,7 @@ extern "C" int laser_experts_down(const void* act, const void* w_down, int32_t T
   clear_stale_error();
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   const hipError_t err = f32 ? launch_experts<true, false, Tile<true, 64, 128, 1, 4, 3>>(a, s)
+                         : a.slots >= 128 * a.E ? launch_experts<false, false, Tile<false, 256, 256, 2, 4, 2>>(a, s)
                              : launch_experts<false, false, Tile<false, 64, 128, 1, 4, 3>>(a, s);
   if (err != hipSuccess) return LASER_E_LAUNCH;
   const size_t quads = (size_t)T * (H / 4);

@@ -23,8 +23,18 @@ typedef unsigned int mma_u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int mma_u32x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) unsigned char* lds_bytes;
 typedef __attribute__((address_space(3))) mma_u32x4* lds_piece;
+typedef __attribute__((address_space(3))) mma_f32x4* lds_f32x4;
+typedef __attribute__((address_space(3))) mma_u32x2* lds_u32x2;
 
 constexpr int kStepBytes = 128;
+struct true_c {
+  static constexpr bool value = true;
+  __device__ constexpr operator bool() const { return true; }
+};
+struct false_c {
+  static constexpr bool value = false;
+  __device__ constexpr operator bool() const { return false; }
+};
 
 // What lanes load whose piece lies behind the end of the rows (both operands then hold zeros).
 static __device__ __align__(16) const unsigned int zero_piece[4] = {0, 0, 0, 0};
@@ -97,32 +107,73 @@ struct Tile {
   __device__ static int row(int wave, int lane, int i) { return (wave + i * kWaves) * 8 + (lane >> 3); }
   __device__ static int piece(int wave, int lane) { return (lane & 7) ^ ((wave & 1) * 4 + (lane >> 4)); }
 
-  // from[i]: where load i of this lane begins (row start + 16 * piece).  `bytes`: length of
-  // the rows, a multiple of 16.  Ends with every wavefront through with its reads of LDS.
-  __device__ static void run(const unsigned char* (&from)[kLoads], int bytes, unsigned lds, int wave, int lane,
-                             mma_f32x4 (&acc)[NB][MB]) {
-    const int steps = (bytes + kStepBytes - 1) / kStepBytes;
-    const bool in_last = piece(wave, lane) * 16 < bytes - (steps - 1) * kStepBytes;
-    const unsigned put = __builtin_amdgcn_readfirstlane(lds + wave * 8 * kStepBytes);
-    auto issue = [&](int step, int slot) {
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        const unsigned char* p = from[i];
-        from[i] += kStepBytes;
-        if (step == steps - 1) p = in_last ? p : reinterpret_cast<const unsigned char*>(zero_piece);
-        load_to_lds(p, put + slot * kStage + i * kWaves * 8 * kStepBytes);
-      }
-    };
-    const int wm = wave % WM, wn = wave / WM;
-    // (piece s * 4 + lane / 16 of row lane % 16, s = 0, 1)
-    const unsigned get = (lane & 15) * kStepBytes + ((lane >> 4) ^ ((lane & 15) >> 1)) * 16;
-    const unsigned get_t = lds + wm * (BM / WM) * kStepBytes + get;
-    const unsigned get_w = lds + (BM + wn * (BN / WN)) * kStepBytes + get;
+  // The product of one tile.  from[i]: where load i of this lane begins (row start + 16 *
+  // piece); `bytes`: length of the rows, a multiple of 16.  start() puts the first steps on
+  // their way to LDS, which nobody may be reading any more; run() does the rest and ends with
+  // every wavefront through with its reads of LDS.
+  int steps;
+  bool in_last;    // whether this lane's piece of the last step is inside the rows
+  unsigned put;    // where this wavefront's loads go in slot 0
+  unsigned get_t, get_w;  // this lane's operands in slot 0, first half of the step
 
+  __device__ Tile(int bytes, unsigned lds, int wave, int lane) {
+    steps = (bytes + kStepBytes - 1) / kStepBytes;
+    in_last = piece(wave, lane) * 16 < bytes - (steps - 1) * kStepBytes;
+    put = __builtin_amdgcn_readfirstlane(lds + wave * 8 * kStepBytes);
+    const unsigned get = (lane & 15) * kStepBytes + ((lane >> 4) ^ ((lane & 15) >> 1)) * 16;
+    get_t = lds + wave % WM * 16 * kStepBytes + get;
+    get_w = lds + (BM + wave / WM * (BN / WN)) * kStepBytes + get;
+  }
+
+  template <typename LAST>
+  __device__ void load(const unsigned char* (&from)[kLoads], LAST last, unsigned slot, int i) const {
+    const unsigned char* p = from[i];
+    from[i] += kStepBytes;
+    if (last) p = in_last ? p : reinterpret_cast<const unsigned char*>(zero_piece);
+    load_to_lds(p, put + slot + i * kWaves * 8 * kStepBytes);
+  }
+  template <typename LAST>
+  __device__ void load_all(const unsigned char* (&from)[kLoads], LAST last, unsigned slot) const {
 #pragma unroll
-    for (int s = 0; s < ST - 1; ++s)
-      if (s < steps) issue(s, s);
-    int slot = 0;
+    for (int i = 0; i < kLoads; ++i) load(from, last, slot, i);
+  }
+  // Blocks of 16 tokens go to the WM wavefronts of a column in turn, so that a tile with few
+  // rows is work for all of them: row of token block m, and how many blocks have rows at all.
+  __device__ static int block_row(int wave, int m) { return (m * WM + wave % WM) * 16; }
+  __device__ static int blocks_of(int wave, int rows) { return ((rows + 15) / 16 - wave % WM + WM - 1) / WM; }
+
+  // operand block m (or n) of half s of the step in `slot`
+  __device__ mma_u32x4 token_block(unsigned slot, int s, int m) const {
+    return read_lds(((get_t + slot) ^ (s * 64)) + m * WM * 16 * kStepBytes);
+  }
+  __device__ mma_u32x4 weight_block(unsigned slot, int s, int n) const {
+    return read_lds(((get_w + slot) ^ (s * 64)) + n * 16 * kStepBytes);
+  }
+
+  __device__ void start(const unsigned char* (&from)[kLoads]) const {
+    constexpr int kAhead = ST == 2 ? 2 : ST - 1;
+#pragma unroll
+    for (int s = 0; s < kAhead; ++s)
+      if (s < steps) load_all(from, s == steps - 1, s * kStage);
+  }
+
+  // start() in two parts: between them only the first half of the ring is being filled
+  __device__ void start_first(const unsigned char* (&from)[kLoads]) const { load_all(from, steps == 1, 0); }
+  __device__ void start_second(const unsigned char* (&from)[kLoads]) const {
+    if (steps > 1) load_all(from, steps == 2, kStage);
+  }
+
+  // `blocks`: this wavefront's token blocks that have rows; the others' products are left out
+  __device__ void run(const unsigned char* (&from)[kLoads], int blocks, mma_f32x4 (&acc)[NB][MB]) const {
+    if constexpr (ST == 2)
+      run_interleaved(from, blocks, acc);
+    else
+      run_ring(from, blocks, acc);
+    lds_barrier();
+  }
+
+  __device__ void run_ring(const unsigned char* (&from)[kLoads], int blocks, mma_f32x4 (&acc)[NB][MB]) const {
+    unsigned slot = 0;
     for (int step = 0; step < steps; ++step) {
       // this wavefront's loads of the step are there, and its reads of the step before
       // are done, for which the slot that is loaded next was waiting
@@ -130,24 +181,134 @@ struct Tile {
         asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((ST - 2) * kLoads) : "memory");
       else
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-      if (step + ST - 1 < steps) issue(step + ST - 1, slot == 0 ? ST - 1 : slot - 1);
+      if (step + ST - 1 < steps)
+        load_all(from, step + ST == steps, slot == 0 ? (ST - 1) * kStage : slot - kStage);
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
         mma_u32x4 w[NB], t[MB];
 #pragma unroll
-        for (int n = 0; n < NB; ++n) w[n] = read_lds((get_w + slot * kStage + n * 16 * kStepBytes) ^ (s * 64));
+        for (int n = 0; n < NB; ++n) w[n] = weight_block(slot, s, n);
 #pragma unroll
-        for (int m = 0; m < MB; ++m) t[m] = read_lds((get_t + slot * kStage + m * 16 * kStepBytes) ^ (s * 64));
+        for (int m = 0; m < MB; ++m)
+          if (m < blocks) {
+            t[m] = token_block(slot, s, m);
 #pragma unroll
-        for (int n = 0; n < NB; ++n)
-#pragma unroll
-          for (int m = 0; m < MB; ++m) acc[n][m] = multiply<F32>(w[n], t[m], acc[n][m]);
+            for (int n = 0; n < NB; ++n) acc[n][m] = multiply<F32>(w[n], t[m], acc[n][m]);
+          }
       }
-      slot = slot == ST - 1 ? 0 : slot + 1;
+      slot = slot == (ST - 1) * kStage ? 0 : slot + kStage;
     }
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  }
+
+  // Two slots, and a fixed order of everything within a step: 2 MB groups of NB products that
+  // share a token block, each with one read from LDS for the group kAhead later and, behind the
+  // barrier, one load of the step after the next.  The barrier lies where the last read of the
+  // step's slot has been made, kAhead groups before its products are; what follows it reads the
+  // other slot and refills this one.  (Left to itself the compiler puts the reads of half a
+  // step right before their use, where both wavefronts of a SIMD wait for them at once: 8192 x
+  // 8192 x 4096 in bf16 took 462 us instead of 387, with one more memory round trip exposed per
+  // step; the matrix instructions alone, on the same operands, take 345: the card lowers its
+  // clock under them.  Loads in bursts of two per group: 404; the barrier two groups later: 394.)
+  __device__ void run_interleaved(const unsigned char* (&from)[kLoads], int blocks, mma_f32x4 (&acc)[NB][MB]) const {
+    constexpr int kGroups = 2 * MB, kAhead = MB - 1;
+    mma_u32x4 w[2][NB], t[MB];
+    unsigned slot = 0;
+    auto step = [&](auto next, auto issued, auto last) {  // `next`: another step follows; `issued`: and one more
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) {
+        const int behind = g - (kGroups - kAhead);  // groups since the barrier
+        if (next && behind == 0) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (behind < 0 || next) {
+          const int r = (g + kAhead) % kGroups;
+          t[r % MB] = token_block(behind < 0 ? slot : slot ^ kStage, r / MB, r % MB);
+        }
+        if (g >= 1 && g <= NB) w[1][g - 1] = weight_block(slot, 1, g - 1);
+        if (next && behind >= 0) {
+#pragma unroll
+          for (int n = 0; n < NB; ++n)
+            if (n * kAhead / NB == behind) w[0][n] = weight_block(slot ^ kStage, 0, n);
+          if constexpr (decltype(issued)::value) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i)
+              if (i * kAhead / kLoads == behind) load(from, last, slot, i);
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (g % MB < blocks)
+#pragma unroll
+          for (int n = 0; n < NB; ++n) acc[n][g % MB] = multiply<F32>(w[g / MB][n], t[g % MB], acc[n][g % MB]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      slot ^= kStage;
+    };
+    static_assert((kStage & (kStage - 1)) == 0 && NB < MB, "slots that differ in one bit; weights of half a step read within it");
+    if (steps > 1)
+      asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kLoads) : "memory");
+    else
+      asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+#pragma unroll
+    for (int n = 0; n < NB; ++n) w[0][n] = weight_block(0, 0, n);
+#pragma unroll
+    for (int g = 0; g < kAhead; ++g) t[g] = token_block(0, 0, g);
+    int left = steps - 1;
+    for (; left > 2; --left) step(true_c{}, true_c{}, false_c{});
+    if (left == 2) step(true_c{}, true_c{}, true_c{}), --left;
+    if (left == 1) step(true_c{}, false_c{}, false_c{});
+    step(false_c{}, false_c{}, false_c{});
   }
 };
+
+// Results -> memory by whole lines: a wavefront puts the blocks of its part of the tile into
+// a piece of LDS of its own (`lds`: the first of them; the second slot of two, or the whole ring), as many token blocks at a time as fit, and reads them back
+// row by row.  value(n, m): the four outputs of column block n < NC that this lane holds;
+// place(row, column): where the 16 bytes beginning at that row and (wavefront's) column go, or
+// NULL.  (Stores straight from the accumulators reach 16 rows with 32 or 64 bytes each:
+// 98304 x 2048 x 1408 in bf16 took 525 us so and 485 this way, with fp32 results 560 and 515,
+// with none 412.  They go past the caches: nobody reads them soon.)
+template <bool F32, class TL, int NC, typename VALUE, typename PLACE>
+__device__ __forceinline__ void store_tile(unsigned lds, int wave, int lane, VALUE value, PLACE place) {
+  constexpr int kBytes = (TL::ST == 2 ? TL::kStage : TL::kLdsBytes) / TL::kWaves;
+  constexpr int kRow = NC * 16 * (F32 ? 4 : 2);                    // bytes of a row
+  constexpr int kFit = kBytes / (16 * kRow);
+  constexpr int kPass = kFit < TL::MB ? kFit : TL::MB;             // token blocks at a time
+  constexpr int kPieces = kRow / 16, kRows = 64 / kPieces;         // pieces of a row; rows per store instruction
+  static_assert(kPass >= 1 && kPass * 16 % kRows == 0 && kPieces <= 16 && (kPieces & (kPieces - 1)) == 0, "whole instructions");
+  const unsigned mine = lds + wave * kBytes;
+  const int tok = lane & 15, quad = lane >> 4;
+  constexpr int kTurn = kPieces - 1;  // (pieces are turned by the row, against bank conflicts)
+#pragma unroll
+  for (int m0 = 0; m0 < TL::MB; m0 += kPass) {
+#pragma unroll
+    for (int m = m0; m < m0 + kPass && m < TL::MB; ++m)
+#pragma unroll
+      for (int n = 0; n < NC; ++n) {
+        const mma_f32x4 v = value(n, m);
+        const unsigned row = mine + ((m - m0) * 16 + tok) * kRow;
+        if constexpr (F32) {
+          *(lds_f32x4)(size_t)(row + ((n * 4 + quad) ^ (tok & kTurn)) * 16) = v;
+        } else {
+          mma_u32x2 b;
+          b[0] = bf16_bits(v[0]) | bf16_bits(v[1]) << 16;
+          b[1] = bf16_bits(v[2]) | bf16_bits(v[3]) << 16;
+          *(lds_u32x2)(size_t)(row + ((n * 2 + (quad >> 1)) ^ (tok & kTurn)) * 16 + (quad & 1) * 8) = b;
+        }
+      }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    constexpr int kStores = kPass * 16 / kRows;
+    mma_u32x4 d[kStores];
+    mma_u32x4* to[kStores];
+#pragma unroll
+    for (int i = 0; i < kStores; ++i) {
+      const int r = i * kRows + lane / kPieces, c = lane % kPieces;
+      to[i] = m0 + r / 16 < TL::MB ? static_cast<mma_u32x4*>(place(TL::block_row(wave, m0 + r / 16) + r % 16, c * (F32 ? 4 : 8))) : nullptr;
+      d[i] = read_lds(mine + r * kRow + (c ^ (r & kTurn)) * 16);
+    }
+#pragma unroll
+    for (int i = 0; i < kStores; ++i)
+      if (to[i] != nullptr) __builtin_nontemporal_store(d[i], to[i]);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  }
+}
 
 // Number `v` of `total` workgroups that the eight XCDs take in turn -> the tile it computes,
 // so that an XCD has one contiguous run of tiles (they share rows through its L2).

@@ -198,6 +198,9 @@ inline hipError_t allow_dynamic_lds(const void* fn, int bytes, LdsAttr& rec) {
 // Analysis workgroups of the persistent gate kernel of pipelined calls: one per compute
 // unit of the current device but the one the chain workgroup occupies (255 if the device
 // cannot be asked).  Cached per device.
+inline int pipeline_workgroups();
+// Compute units of the current device (256 if it cannot be asked).
+inline int compute_units() { return pipeline_workgroups() + 1; }
 inline int pipeline_workgroups() {
   static int cached[kMaxDevices] = {};
   int dev = 0;

@@ -63,7 +63,7 @@ __global__ __launch_bounds__(TL::kThreads) void project_kernel(ProjectArgs a) {
   constexpr int BM = TL::BM, BN = TL::BN, NB = TL::NB, MB = TL::MB;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int nt = (a.N + BN - 1) / BN, total = (a.T + BM - 1) / BM * nt;
-  const int wm = wave % TL::WM, wn = wave / TL::WM;
+  const int wn = wave / TL::WM;
   for (int v = blockIdx.x; v < total; v += gridDim.x) {
     const int id = xcd_run(v, total);
     const int t0 = id / nt * BM, n0 = id % nt * BN;
@@ -79,10 +79,12 @@ __global__ __launch_bounds__(TL::kThreads) void project_kernel(ProjectArgs a) {
     for (int n = 0; n < NB; ++n)
 #pragma unroll
       for (int m = 0; m < MB; ++m) acc[n][m] = mma_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    TL::run(from, a.K, lds, wave, lane, acc);
+    const TL tile(a.K, lds, wave, lane);
+    tile.start(from);
+    tile.run(from, TL::blocks_of(wave, a.T - t0), acc);
 #pragma unroll
     for (int m = 0; m < MB; ++m) {
-      const int t = t0 + wm * (BM / TL::WM) + m * 16 + (lane & 15);
+      const int t = t0 + TL::block_row(wave, m) + (lane & 15);
       if (t >= a.T) continue;
       const int ad = a.adapter[t];
 #pragma unroll
