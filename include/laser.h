@@ -355,7 +355,7 @@ size_t laser_project_workspace_bytes(int32_t T, int32_t H, int32_t N,
  *   workspace        >= laser_project_workspace_bytes(...) bytes, 256-byte aligned
  * a_down, a_up, request_offsets and request_adapters may be NULL if there are no adapters
  * or no requests.  H a multiple of 8 (bf16) or 4 (fp32), matrices 16-byte aligned and
- * without gaps between rows; N is free.
+ * without gaps between rows; N is free; T <= 2^27.
  */
 int laser_project_adapted(const void* x, const void* w, int32_t T, int32_t H, int32_t N,
                           const laser_adapter_params_t* params, const void* a_down,

@@ -1,5 +1,14 @@
 // A projection that all rows of a batch share, and beside it the low-rank adapters that the
 // requests of the batch bring along: laser_project_adapted.
+//
+//   out[t, :] = W x_t + U_m (scale_m D_m x_t),   m the adapter of row t's request
+//
+// Two launches.  Of few rows and columns ("thin", see launch_project): sums over parts of the
+// contraction axis, of W and of the adapters side by side, then a join.  Else: the inner values
+// v = scale D x of all rows, then the shared product with U v added to its accumulators.
+//
+// v stays in fp32 quality up to the second product: bf16 calls hand it over in three bf16 values
+// that add up to it (8 + 8 + 8 bits), each multiplied by U on its own.
 #include "../../include/laser.h"
 #include "grouped.h"
 
@@ -14,45 +23,255 @@ struct ProjectArgs {
   const int32_t* request_offsets;
   const int32_t* request_adapters;
   void* out;               // [T, N]
-  float* inner;            // [T, R]  scale * (A x) of the row's adapter
-  int32_t* adapter;        // [T]     the row's adapter, or -1
+  void* inner;             // v: [T, 3, R] bf16 or [T, R] fp32;  thin: [slices, T, R] fp32, not scaled
+  float* shared;           // thin: [slices, T, N]
+  int32_t* adapter;        // [T] the row's adapter, or -1
   int T, N, M, R, requests;
-  int H;
   int K;                   // bytes of a row of x, w and a_down
+  int lanes;               // workgroups that share the distinct adapters of 16 rows
+  int slices;              // parts of the contraction axis (thin)
 };
 
-// The adapter of row t (or -1): the last request that begins at or before t, if t is still in it.
-__device__ __forceinline__ int adapter_of(const ProjectArgs& a, int t) {
-  int lo = 0, hi = a.requests;  // request_offsets[lo - 1] <= t < request_offsets[hi], were there one
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (a.request_offsets[mid] <= t) lo = mid + 1; else hi = mid;
+// How many of request_offsets[0 .. requests - 1] are <= t; the same t in all lanes.
+__device__ __forceinline__ int requests_begun(const ProjectArgs& a, int t, int lane) {
+  int lo = 0, len = a.requests;
+  while (len > 64) {  // 64 probes at a time
+    const int gap = (len + 63) >> 6, at = lane * gap;
+    const int below = __popcll(__ballot(at < len && a.request_offsets[lo + min(at, len - 1)] <= t));
+    if (below == 0) return lo;
+    lo += (below - 1) * gap + 1;
+    len = min(gap - 1, len - (below - 1) * gap - 1);
   }
-  if (lo == 0 || t >= a.request_offsets[lo]) return -1;
-  const int m = a.request_adapters[lo - 1];
+  return lo + __popcll(__ballot(lane < len && a.request_offsets[lo + min(lane, max(len - 1, 0))] <= t));
+}
+
+// The adapter of row t0 + lane % 16, or -1.
+__device__ __forceinline__ int adapter_of_row(const ProjectArgs& a, int t0, int lane) {
+  if (a.requests == 0) return -1;
+  const int t = t0 + (lane & 15);
+  const int first = requests_begun(a, t0, lane);
+  // the requests that begin behind t0: 64 at a time
+  int begun = first;
+  for (int at = first; at < a.requests; at += 64) {
+    const int start = at + lane < a.requests ? a.request_offsets[at + lane] : 0x7fffffff;
+    if (__ballot(start <= t0 + 15) == 0) break;
+#pragma unroll
+    for (int i = 1; i < 16; ++i) {
+      const int n = __popcll(__ballot(start <= t0 + i));
+      if ((lane & 15) == i) begun += n;
+    }
+  }
+  if (begun == 0 || t >= a.T || t >= a.request_offsets[begun]) return -1;
+  const int m = a.request_adapters[begun - 1];
   return (unsigned)m < (unsigned)a.M ? m : -1;
 }
 
-// inner[t, r] = scale * sum_h A[r, h] x[t, h]: one wavefront per row.
-template <bool F32>
-__global__ __launch_bounds__(256) void adapter_inner_kernel(ProjectArgs a) {
-  const int lane = threadIdx.x & 63, t = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (t >= a.T) return;
-  const int m = adapter_of(a, t);
-  if (lane == 0) a.adapter[t] = m;
-  if (m < 0) return;
-  const float scale = a.scales != nullptr ? a.scales[m] : 1.0f;
-  for (int r = 0; r < a.R; ++r) {
-    float sum = 0.0f;
-    for (int h = lane * 4; h < a.H; h += 256) {
-      const mma_f32x4 x = load4<F32>(a.x, (size_t)t * a.H + h);
-      const mma_f32x4 w = load4<F32>(a.a_down, ((size_t)m * a.R + r) * a.H + h);
+// acc[b] += rows (16 b + lane % 16) of `rows` times the 16 token rows, columns of k-steps (64
+// bytes) from `begin` to `end`.  Operands go memory -> registers, four steps in flight.
+template <bool F32, int B>
+__device__ __forceinline__ void thin_product(const unsigned char* tokens, const unsigned char* const (&rows)[B], int bytes,
+                                             int begin, int end, int lane, mma_f32x4 (&acc)[B]) {
+  const int own = (lane >> 4) * 16;
+  constexpr int kBatch = B <= 2 ? 4 : 2;
+  for (int k = begin; k < end; k += kBatch) {
+    mma_u32x4 t[kBatch], r[kBatch][B];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) sum = fmaf(x[i], w[i], sum);
+    for (int i = 0; i < kBatch; ++i) {
+      const int at = (k + i) * 64 + own;
+      const bool in = k + i < end && at < bytes;
+      const int from = in ? at : 0;
+      t[i] = *reinterpret_cast<const mma_u32x4*>(tokens + from);
+#pragma unroll
+      for (int b = 0; b < B; ++b) r[i][b] = *reinterpret_cast<const mma_u32x4*>(rows[b] + from);
+      if (!in) {  // both operands: what lies there may be anything
+        t[i] = mma_u32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int b = 0; b < B; ++b) r[i][b] = mma_u32x4{0, 0, 0, 0};
+      }
     }
 #pragma unroll
-    for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-    if (lane == 0) a.inner[(size_t)t * a.R + r] = sum * scale;
+    for (int i = 0; i < kBatch; ++i)
+#pragma unroll
+      for (int b = 0; b < B; ++b) acc[b] = multiply<F32>(r[i][b], t[i], acc[b]);
+  }
+}
+
+// The four wavefronts' sums of B blocks, added in their order; value i of thread j is row
+// 4 (lane / 16) + i, token lane % 16 of block wave + 4 n.
+template <int B, typename USE>
+__device__ __forceinline__ void join_wavefronts(mma_f32x4 (&acc)[B], float* part, int wave, int lane, USE use) {
+#pragma unroll
+  for (int b = 0; b < B; ++b) *reinterpret_cast<mma_f32x4*>(part + ((b * 4 + wave) * 64 + lane) * 4) = acc[b];
+  __syncthreads();
+  for (int b = wave; b < B; b += 4) {
+    mma_f32x4 sum = *reinterpret_cast<const mma_f32x4*>(part + (b * 4 * 64 + lane) * 4);
+#pragma unroll
+    for (int w = 1; w < 4; ++w) sum += *reinterpret_cast<const mma_f32x4*>(part + ((b * 4 + w) * 64 + lane) * 4);
+    use(b, sum);
+  }
+  __syncthreads();
+}
+
+// x = hi + mid + lo, three bf16 values
+__device__ __forceinline__ void split3(float x, unsigned (&piece)[3]) {
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    piece[i] = bf16_bits(x);
+    x -= bf16_value(piece[i]);
+  }
+}
+
+// Workgroup (x, y, z): 16 rows, every lanes-th of their distinct adapters from y on, slice z of
+// the contraction axis, cut over the four wavefronts.  THIN: sums of slices, and behind the
+// first `lanes` y the shared projection, 16 columns each.
+template <bool F32, int B, bool THIN>
+__global__ __launch_bounds__(256) void adapter_inner_kernel(ProjectArgs a) {
+  __shared__ __align__(16) float part[B * 4 * 256];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int t0 = blockIdx.x * 16, t = t0 + (lane & 15);
+  const int steps = (a.K + 63) >> 6, parts = 4 * (THIN ? a.slices : 1), own = (THIN ? 4 * (int)blockIdx.z : 0) + wave;
+  const int begin = (int)((long long)steps * own / parts), end = (int)((long long)steps * (own + 1) / parts);
+  const unsigned char* const tokens = a.x + (size_t)min(t, a.T - 1) * a.K;
+  if (THIN && (int)blockIdx.y >= a.lanes) {
+    const int n0 = (blockIdx.y - a.lanes) * 16;
+    const unsigned char* rows[1] = {a.w + (size_t)min(n0 + (lane & 15), a.N - 1) * a.K};
+    mma_f32x4 acc[1] = {mma_f32x4{0.0f, 0.0f, 0.0f, 0.0f}};
+    thin_product<F32, 1>(tokens, rows, a.K, begin, end, lane, acc);
+    join_wavefronts<1>(acc, part, wave, lane, [&](int, mma_f32x4 sum) {
+      if (t >= a.T) return;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int n = n0 + 4 * (lane >> 4) + i;
+        if (n < a.N) a.shared[((size_t)blockIdx.z * a.T + t) * a.N + n] = sum[i];
+      }
+    });
+    return;
+  }
+  const int m = adapter_of_row(a, t0, lane);
+  if (blockIdx.y == 0 && blockIdx.z == 0 && threadIdx.x < 16 && t < a.T) a.adapter[t] = m;
+  unsigned todo = (unsigned)__ballot(m >= 0) & 0xffffu;
+  for (int nth = 0; todo != 0; ++nth) {
+    const int ad = __builtin_amdgcn_readlane(m, __builtin_ctz(todo));
+    const bool mine = m == ad;
+    todo &= ~(unsigned)__ballot(mine);
+    if (nth % a.lanes != (int)blockIdx.y) continue;
+    const unsigned char* rows[B];
+#pragma unroll
+    for (int b = 0; b < B; ++b) rows[b] = a.a_down + ((size_t)ad * a.R + min(b * 16 + (lane & 15), a.R - 1)) * a.K;
+    mma_f32x4 acc[B];
+#pragma unroll
+    for (int b = 0; b < B; ++b) acc[b] = mma_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    thin_product<F32, B>(tokens, rows, a.K, begin, end, lane, acc);
+    const float scale = THIN || a.scales == nullptr ? 1.0f : a.scales[ad];
+    join_wavefronts<B>(acc, part, wave, lane, [&](int b, mma_f32x4 sum) {
+      const int r = b * 16 + 4 * (lane >> 4);
+      if (!mine || r >= a.R) return;  // (R is a multiple of 4)
+      if constexpr (THIN || F32) {
+        store4<true>(a.inner, ((THIN ? (size_t)blockIdx.z * a.T : 0) + t) * a.R + r, sum * scale);
+      } else {
+        unsigned p[4][3];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) split3(sum[i] * scale, p[i]);
+#pragma unroll
+        for (int j = 0; j < 3; ++j)
+          *reinterpret_cast<mma_u32x2*>(static_cast<unsigned short*>(a.inner) + ((size_t)t * 3 + j) * a.R + r) =
+              mma_u32x2{p[0][j] | p[1][j] << 16, p[2][j] | p[3][j] << 16};
+      }
+    });
+  }
+}
+
+// Thin calls, second launch: one workgroup per row and 256 columns.
+template <bool F32, bool OUT32>
+__global__ __launch_bounds__(256) void adapter_join_kernel(ProjectArgs a) {
+  __shared__ float v[LASER_MAX_RANK];
+  const int t = blockIdx.x, n = blockIdx.y * 256 + threadIdx.x;
+  const int m = a.adapter[t];
+  if (m >= 0 && (int)threadIdx.x < a.R) {
+    float sum = 0.0f;
+    for (int s = 0; s < a.slices; ++s) sum += static_cast<const float*>(a.inner)[((size_t)s * a.T + t) * a.R + threadIdx.x];
+    v[threadIdx.x] = sum * (a.scales != nullptr ? a.scales[m] : 1.0f);
+  }
+  float y = 0.0f;
+  if (n < a.N)
+    for (int s = 0; s < a.slices; ++s) y += a.shared[((size_t)s * a.T + t) * a.N + n];
+  __syncthreads();
+  if (n >= a.N) return;
+  if (m >= 0) {
+    const size_t row = ((size_t)m * a.N + n) * a.R;
+    float d = 0.0f;
+    for (int r = 0; r < a.R; r += 4) {
+      const mma_f32x4 u = load4<F32>(a.a_up, row + r);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) d = fmaf(u[i], v[r + i], d);
+    }
+    y += d;
+  }
+  const size_t at = (size_t)t * a.N + n;
+  if constexpr (OUT32) static_cast<float*>(a.out)[at] = y;
+  else static_cast<unsigned short*>(a.out)[at] = (unsigned short)bf16_bits(y);
+}
+
+// U v added to a wavefront's accumulators: per block of 16 tokens and distinct adapter in it, 32
+// values of v at a time (fp32: 16), the rows of other adapters as zeros.
+template <bool F32, class TL>
+__device__ __forceinline__ void add_adapters(const ProjectArgs& a, int t0, int n0, int blocks, int wave, int lane,
+                                             mma_f32x4 (&acc)[TL::NB][TL::MB]) {
+  constexpr int NB = TL::NB, MB = TL::MB, kPieces = F32 ? 1 : 3;
+  constexpr int kSize = F32 ? 4 : 2, kOwn = 16 / kSize;  // values of v that a lane holds at a time
+  int ids[MB];
+  bool any = false;
+#pragma unroll
+  for (int m = 0; m < MB; ++m) {
+    const int t = t0 + TL::block_row(wave, m) + (lane & 15);
+    ids[m] = t < a.T ? a.adapter[t] : -1;
+    any |= ids[m] >= 0;
+  }
+  if (__ballot(any) == 0) return;
+  for (int r0 = 0; r0 < a.R; r0 += 4 * kOwn) {
+    const int r = r0 + (lane >> 4) * kOwn;
+    const bool in = r < a.R;
+    int held = -1;  // the adapter whose rows are in u
+    mma_u32x4 u[NB];
+#pragma unroll
+    for (int m = 0; m < MB; ++m) {
+      unsigned todo = (unsigned)__ballot(ids[m] >= 0) & 0xffffu;
+      if (todo == 0) continue;
+      const int t = min(t0 + TL::block_row(wave, m) + (lane & 15), a.T - 1);
+      mma_u32x4 v[kPieces];
+#pragma unroll
+      for (int j = 0; j < kPieces; ++j)
+        v[j] = *reinterpret_cast<const mma_u32x4*>(static_cast<const unsigned char*>(a.inner) +
+                                                   (((size_t)t * kPieces + j) * a.R + (in ? r : 0)) * kSize);
+      while (todo != 0) {
+        const int ad = __builtin_amdgcn_readlane(ids[m], __builtin_ctz(todo));
+        const bool mine = ids[m] == ad;
+        todo &= ~(unsigned)__ballot(mine);
+        if (ad != held) {
+          held = ad;
+#pragma unroll
+          for (int n = 0; n < NB; ++n) {
+            const int row = min(n0 + n * 16 + (lane & 15), a.N - 1);
+            u[n] = *reinterpret_cast<const mma_u32x4*>(a.a_up + (((size_t)ad * a.N + row) * a.R + (in ? r : 0)) * kSize);
+            if (!in) u[n] = mma_u32x4{0, 0, 0, 0};
+          }
+        }
+        mma_f32x4 d[NB];
+#pragma unroll
+        for (int n = 0; n < NB; ++n) d[n] = mma_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int j = kPieces - 1; j >= 0; --j) {
+          const mma_u32x4 b = mine && in ? v[j] : mma_u32x4{0, 0, 0, 0};
+#pragma unroll
+          for (int n = 0; n < NB; ++n) d[n] = multiply<F32>(u[n], b, d[n]);
+        }
+        // (not added to rows of other adapters: a zero times an infinity in u is no zero)
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[n][m][i] += mine ? d[n][i] : 0.0f;
+      }
+    }
   }
 }
 
@@ -62,86 +281,140 @@ __global__ __launch_bounds__(TL::kThreads) void project_kernel(ProjectArgs a) {
   const unsigned lds = (unsigned)(size_t)(lds_bytes)ring;
   constexpr int BM = TL::BM, BN = TL::BN, NB = TL::NB, MB = TL::MB;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int nt = (a.N + BN - 1) / BN, total = (a.T + BM - 1) / BM * nt;
+  const int nt = (a.N + BN - 1) / BN, mt = (a.T + BM - 1) / BM, total = mt * nt;
   const int wn = wave / TL::WM;
+  const TL tile(a.K, lds, wave, lane);
   for (int v = blockIdx.x; v < total; v += gridDim.x) {
     const int id = xcd_run(v, total);
-    const int t0 = id / nt * BM, n0 = id % nt * BN;
+    constexpr int kGroup = 8;
+    const int g = id / (kGroup * nt), gm = min(kGroup, mt - g * kGroup), in = id - g * kGroup * nt;
+    const int t0 = (g * kGroup + in % gm) * BM, n0 = in / gm * BN + wn * (BN / TL::WN);
     const unsigned char* from[TL::kLoads];
     const int piece = TL::piece(wave, lane) * 16;
 #pragma unroll
     for (int i = 0; i < TL::kLoads; ++i) {
       const int r = TL::row(wave, lane, i);
-      from[i] = (r < BM ? a.x + (size_t)min(t0 + r, a.T - 1) * a.K : a.w + (size_t)min(n0 + r - BM, a.N - 1) * a.K) + piece;
+      from[i] = (r < BM ? a.x + (size_t)min(t0 + r, a.T - 1) * a.K
+                        : a.w + (size_t)min(in / gm * BN + r - BM, a.N - 1) * a.K) + piece;
     }
     mma_f32x4 acc[NB][MB];
 #pragma unroll
     for (int n = 0; n < NB; ++n)
 #pragma unroll
       for (int m = 0; m < MB; ++m) acc[n][m] = mma_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    const TL tile(a.K, lds, wave, lane);
+    const int rows = min(a.T - t0, BM), blocks = TL::blocks_of(wave, rows);
     tile.start(from);
-    tile.run(from, TL::blocks_of(wave, a.T - t0), acc);
+    tile.run(from, blocks, acc);
+    int l = lane;
+    asm volatile("" : "+v"(l));
+    add_adapters<F32, TL>(a, t0, n0, blocks, wave, l, acc);
+    constexpr int kSize = OUT32 ? 4 : 2;
+    if (a.N % (16 / kSize) == 0) {
+      store_tile<OUT32, TL, NB>(
+          lds, wave, l, [&](int n, int m) { return acc[n][m]; },
+          [&](int r, int c) -> void* {
+            return r < rows && n0 + c < a.N ? static_cast<char*>(a.out) + ((size_t)(t0 + r) * a.N + n0 + c) * kSize : nullptr;
+          });
+    } else {
 #pragma unroll
-    for (int m = 0; m < MB; ++m) {
-      const int t = t0 + TL::block_row(wave, m) + (lane & 15);
-      if (t >= a.T) continue;
-      const int ad = a.adapter[t];
+      for (int m = 0; m < MB; ++m) {
+        const int r = TL::block_row(wave, m) + (l & 15);
 #pragma unroll
-      for (int n = 0; n < NB; ++n) {
-        const int c = n0 + wn * (BN / TL::WN) + n * 16 + 4 * (lane >> 4);
+        for (int n = 0; n < NB; ++n)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (c + i >= a.N) continue;
-          float y = 0.0f;
-          if (ad >= 0) {
-            const size_t row = ((size_t)ad * a.N + c + i) * a.R;
-            for (int r = 0; r < a.R; r += 4) {
-              const mma_f32x4 b = load4<F32>(a.a_up, row + r);
-#pragma unroll
-              for (int j = 0; j < 4; ++j) y = fmaf(b[j], a.inner[(size_t)t * a.R + r + j], y);
-            }
+          for (int i = 0; i < 4; ++i) {
+            const int c = n0 + n * 16 + 4 * (l >> 4) + i;
+            const size_t at = (size_t)(t0 + r) * a.N + c;
+            if (r >= rows || c >= a.N) continue;
+            if constexpr (OUT32) static_cast<float*>(a.out)[at] = acc[n][m][i];
+            else static_cast<unsigned short*>(a.out)[at] = (unsigned short)bf16_bits(acc[n][m][i]);
           }
-          y += acc[n][m][i];
-          const size_t at = (size_t)t * a.N + c + i;
-          if constexpr (OUT32) static_cast<float*>(a.out)[at] = y;
-          else static_cast<unsigned short*>(a.out)[at] = (unsigned short)bf16_bits(y);
-        }
       }
     }
+    lds_barrier();  // (the ring is free again)
   }
 }
 
-static size_t inner_bytes(int32_t T, const laser_adapter_params_t* p) { return ((size_t)T * p->rank * 4 + 255) & ~(size_t)255; }
+// ---- host ---------------------------------------------------------------------------
+
+constexpr int kThinSlices = 8;
+constexpr int kThinRows = 512, kThinValues = 1 << 16;
+static bool is_thin(int T, int N) { return T <= kThinRows && (long long)T * N <= kThinValues; }
+
+static size_t whole(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
+struct ProjectLayout {
+  size_t adapter, inner, shared, total;
+};
+static ProjectLayout project_layout(int T, int N, const laser_adapter_params_t* p) {
+  const bool thin = is_thin(T, N);
+  const size_t per_value = thin ? 4 * kThinSlices : p->dtype == LASER_DTYPE_F32 ? 4 : 6;
+  ProjectLayout L;
+  L.adapter = 0;
+  L.inner = whole((size_t)T * 4);
+  L.shared = L.inner + whole((size_t)T * p->rank * per_value);
+  L.total = L.shared + (thin ? whole((size_t)T * N * 4 * kThinSlices) : 0) + 256;
+  return L;
+}
 
 static int check_project(int32_t T, int32_t H, int32_t N, const laser_adapter_params_t* p) {
   if (!p) return LASER_E_NULL;
   if (p->struct_bytes != sizeof(laser_adapter_params_t)) return LASER_E_STRUCT;
   if (T < 0 || H < 1 || N < 1 || p->adapters < 0 || p->requests < 0) return LASER_E_RANGE;
-  if (T > (1 << 30) || H > (1 << 28) || N > (1 << 28)) return LASER_E_RANGE;
+  if (T > (1 << 27) || H > (1 << 28) || N > (1 << 28)) return LASER_E_RANGE;
   if (p->dtype != LASER_DTYPE_F32 && p->dtype != LASER_DTYPE_BF16) return LASER_E_RANGE;
   if (p->out_dtype != LASER_DTYPE_F32 && p->out_dtype != p->dtype) return LASER_E_RANGE;
   if (p->rank < 1) return LASER_E_RANGE;
   if (p->rank > LASER_MAX_RANK) return LASER_E_UNSUPPORTED;
-  const int whole = p->dtype == LASER_DTYPE_F32 ? 4 : 8;
-  if (H % whole != 0 || p->rank % whole != 0) return LASER_E_ALIGN;
+  const int pieces = p->dtype == LASER_DTYPE_F32 ? 4 : 8;
+  if (H % pieces != 0 || p->rank % pieces != 0) return LASER_E_ALIGN;
   return LASER_OK;
 }
 
-template <bool F32, bool OUT32>
-static hipError_t launch_project(const ProjectArgs& a, hipStream_t s) {
-  using TL = Tile<F32, 64, 64, 1, 4, 3>;
+template <bool F32, bool THIN>
+static hipError_t launch_inner(const ProjectArgs& a, dim3 grid, hipStream_t s) {
+  if (a.R <= 16)
+    hipLaunchKernelGGL((adapter_inner_kernel<F32, 1, THIN>), grid, dim3(256), 0, s, a);
+  else if (a.R <= 32)
+    hipLaunchKernelGGL((adapter_inner_kernel<F32, 2, THIN>), grid, dim3(256), 0, s, a);
+  else if (a.R <= 64)
+    hipLaunchKernelGGL((adapter_inner_kernel<F32, 4, THIN>), grid, dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL((adapter_inner_kernel<F32, 8, THIN>), grid, dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+template <bool F32, bool OUT32, class TL>
+static hipError_t launch_tiles(const ProjectArgs& a, hipStream_t s) {
   static LdsAttr attr;
   const void* fn = reinterpret_cast<const void*>(&project_kernel<F32, OUT32, TL>);
   hipError_t err = allow_dynamic_lds(fn, TL::kLdsBytes, attr);
-  if (err != hipSuccess) return err;
-  hipLaunchKernelGGL((adapter_inner_kernel<F32>), dim3((a.T + 3) / 4), dim3(256), 0, s, a);
-  err = hipGetLastError();
   if (err != hipSuccess) return err;
   const long long grid = (long long)((a.T + TL::BM - 1) / TL::BM) * ((a.N + TL::BN - 1) / TL::BN);
   hipLaunchKernelGGL((project_kernel<F32, OUT32, TL>), dim3((unsigned)min(grid, 1ll << 20)), dim3(TL::kThreads),
                      TL::kLdsBytes, s, a);
   return hipGetLastError();
+}
+
+template <bool F32, bool OUT32>
+static hipError_t launch_project(ProjectArgs& a, hipStream_t s) {
+  const int rows16 = (a.T + 15) / 16;
+  if (is_thin(a.T, a.N)) {
+    const int steps = (a.K + 63) / 64;
+    a.slices = min(kThinSlices, max(1, steps / 8));
+    a.lanes = a.requests > 0 ? min(16, a.requests) : 1;
+    hipError_t err = launch_inner<F32, true>(a, dim3(rows16, a.lanes + (a.N + 15) / 16, a.slices), s);
+    if (err != hipSuccess) return err;
+    hipLaunchKernelGGL((adapter_join_kernel<F32, OUT32>), dim3(a.T, (a.N + 255) / 256), dim3(256), 0, s, a);
+    return hipGetLastError();
+  }
+  a.slices = 1;
+  a.lanes = a.requests > 0 ? min(min(16, a.requests), max(1, 1024 / rows16)) : 1;
+  hipError_t err = launch_inner<F32, false>(a, dim3(rows16, a.lanes, 1), s);
+  if (err != hipSuccess) return err;
+  if constexpr (!F32)
+    if ((long long)((a.T + 255) / 256) * ((a.N + 255) / 256) >= compute_units() / 2)
+      return launch_tiles<F32, OUT32, Tile<F32, 256, 256, 2, 4, 2>>(a, s);
+  return launch_tiles<F32, OUT32, Tile<F32, 64, 64, 1, 4, 4>>(a, s);
 }
 
 }  // namespace laser
@@ -150,7 +423,9 @@ using namespace laser;
 
 extern "C" size_t laser_project_workspace_bytes(int32_t T, int32_t H, int32_t N, const laser_adapter_params_t* params) {
   if (check_project(T, H, N, params) != LASER_OK) return 0;
-  return inner_bytes(T, params) + (((size_t)T * 4 + 256) & ~(size_t)255);
+  // (a thin call may need more than one of more rows)
+  const int thin = min(T, min(kThinRows, kThinValues / N));
+  return max(project_layout(T, N, params).total, project_layout(thin, N, params).total);
 }
 
 extern "C" int laser_project_adapted(const void* x, const void* w, int32_t T, int32_t H, int32_t N,
@@ -166,8 +441,10 @@ extern "C" int laser_project_adapted(const void* x, const void* w, int32_t T, in
   if (requests > 0 && (!a_down || !a_up || !request_offsets || !request_adapters)) return LASER_E_NULL;
   const uintptr_t bits = (uintptr_t)x | (uintptr_t)w | (uintptr_t)a_down | (uintptr_t)a_up | (uintptr_t)out;
   if (bits & 15 || (uintptr_t)workspace & 255) return LASER_E_ALIGN;
-  if (workspace_bytes < laser_project_workspace_bytes(T, H, N, params)) return LASER_E_WORKSPACE;
+  const ProjectLayout L = project_layout(T, N, params);
+  if (workspace_bytes < L.total) return LASER_E_WORKSPACE;
   const bool f32 = params->dtype == LASER_DTYPE_F32;
+  char* const ws = static_cast<char*>(workspace);
   ProjectArgs a = {};
   a.x = static_cast<const unsigned char*>(x);
   a.w = static_cast<const unsigned char*>(w);
@@ -177,14 +454,14 @@ extern "C" int laser_project_adapted(const void* x, const void* w, int32_t T, in
   a.request_offsets = request_offsets;
   a.request_adapters = request_adapters;
   a.out = out;
-  a.inner = static_cast<float*>(workspace);
-  a.adapter = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + inner_bytes(T, params));
+  a.inner = ws + L.inner;
+  a.shared = reinterpret_cast<float*>(ws + L.shared);
+  a.adapter = reinterpret_cast<int32_t*>(ws + L.adapter);
   a.T = T;
   a.N = N;
   a.M = params->adapters;
   a.R = params->rank;
   a.requests = requests;
-  a.H = H;
   a.K = H * (f32 ? 4 : 2);
   clear_stale_error();
   hipStream_t s = static_cast<hipStream_t>(hip_stream);

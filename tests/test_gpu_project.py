@@ -28,6 +28,10 @@ SHAPES = [
     (1500, 520, 64, 16, 4, [500, 499, 501]),
     (2100, 136, 264, 64, 3, [2100]),
     (40, 64, 16, 8, 1, []),                         # no requests
+    (513, 136, 24, 24, 700, [1] * 300 + [0, 0] * 100 + [3] * 71),   # hundreds of requests, many of them empty
+    (600, 136, 130, 104, 5, [0] * 70 + [5] * 40 + [0] * 5000 + [400]),
+    (4200, 200, 2061, 40, 6, [900, 20, 1, 2000, 1279]),              # the widest tiles, odd columns
+    (4100, 72, 2560, 128, 3, [1024, 1, 3075]),
 ]
 
 
@@ -76,7 +80,7 @@ def test_rows_before_the_first_request():
     assert not torch.equal(out[17:57], none[17:57])
 
 
-@pytest.mark.parametrize("T,H,N", [(20, 72, 64), (400, 200, 96)])
+@pytest.mark.parametrize("T,H,N", [(20, 72, 64), (400, 200, 96), (1500, 136, 64), (8200, 136, 2056)])
 def test_what_does_not_belong_to_a_row_does_not_reach_it(T, H, N):
     """Infinities and NaN in other rows, in adapters of other requests and in unused ones."""
     half = T // 2
@@ -122,6 +126,15 @@ def test_rows_beyond_four_gigabytes():
     rows = x[torch.from_numpy(some).cuda()].cpu()
     want, tol = P.project_reference(rows, i["w"], i["a_down"], i["a_up"], i["scales"], [0, 5, 7], [1, 0], F32, BF16)
     P.assert_within(P.f64(out[torch.from_numpy(some).cuda()]), want, tol, "far rows")
+
+
+def test_the_workspace_serves_every_smaller_call():
+    """Few rows may need more workspace than many: the size for T covers both."""
+    for N in (1, 64, 130, 5000, 200_000):
+        for R, dtype in ((8, BF16), (128, BF16), (64, F32)):
+            p = B.make_adapter_params(R, 2, 3, dtype=dtype)
+            sizes = [B.laser_project_workspace_bytes(T, 64, N, p) for T in (0, 1, 12, 13, 512, 513, 1024, 1025, 5000)]
+            assert sizes == sorted(sizes)
 
 
 def test_the_gate_of_a_batch_of_adapted_requests():
