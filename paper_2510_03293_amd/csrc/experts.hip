@@ -22,7 +22,7 @@ struct ExpertArgs {
 // Which expert tile `mt` of BM rows belongs to: per lane one expert, tiles counted in order.
 struct ExpertTiles {
   int lo, cnt, before, total;  // this lane's expert: first position, positions, tiles of earlier experts
-  __device__ void init(const ExpertArgs& a, int lane, int BM) {
+  __device__ void init(const ExpertArgs& a, int lane) {
     if (a.offsets == nullptr) {
       lo = 0;
       cnt = lane == 0 ? a.slots : 0;
@@ -31,6 +31,8 @@ struct ExpertTiles {
       lo = lane < a.E ? min(max(a.offsets[lane], 0), a.slots) : 0;
       cnt = lane < a.E ? max(min(a.offsets[lane + 1], a.slots) - lo, 0) : 0;
     }
+  }
+  __device__ void count(int lane, int BM) {
     const int tiles = (cnt + BM - 1) / BM;
     int sum = tiles;
 #pragma unroll
@@ -61,16 +63,13 @@ __device__ __forceinline__ float silu(float g) {
 // the one before is computed: its rows' entries of the permutation before run(), its first
 // steps before the results are written.
 template <bool F32, bool UP, class TL>
-__global__ __launch_bounds__(TL::kThreads) void experts_kernel(ExpertArgs a) {
-  extern __shared__ __align__(1024) unsigned char ring[];
+__device__ __forceinline__ void experts_tiles(const ExpertArgs& a, unsigned char* ring, ExpertTiles tiles, int lane, int wave) {
   constexpr int BM = TL::BM, BN = TL::BN, NB = TL::NB, MB = TL::MB;
   static_assert(BM <= TL::kThreads, "one thread per row of the tile");
   // behind the ring: per row of the tile its token (UP) or its slot and weight
   int* const row_of = reinterpret_cast<int*>(ring + TL::kLdsBytes);
   float* const weight_of = reinterpret_cast<float*>(row_of + 2 * BM);
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  ExpertTiles tiles;
-  tiles.init(a, lane, BM);
+  tiles.count(lane, BM);
   constexpr int kCols = UP ? BN / 2 : BN;  // output columns of a tile
   constexpr int kWaveCols = kCols / TL::WN;
   const int cols = UP ? a.F : a.H;
@@ -190,8 +189,170 @@ __global__ __launch_bounds__(TL::kThreads) void experts_kernel(ExpertArgs a) {
   }
 }
 
+// How many rows the call's experts have is known on the device only: a call that may have either
+// many or few per expert (`rows`: the number from which they are many, 0: no question) is launched
+// with wide tiles and with narrow ones, and one of the two launches finds that it is not meant.
+template <bool F32, bool UP, class TL, bool MANY>
+__global__ __launch_bounds__(TL::kThreads) void experts_kernel(ExpertArgs a, int rows) {
+  extern __shared__ __align__(1024) unsigned char ring[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  ExpertTiles tiles;
+  tiles.init(a, lane);
+  if (rows != 0) {
+    tiles.count(lane, 1);
+    if ((tiles.total >= (long long)rows * __popcll(__ballot(tiles.cnt > 0))) != MANY) return;
+  }
+  experts_tiles<F32, UP, TL>(a, ring, tiles, lane, wave);
+}
+
+// ---- a few tokens -------------------------------------------------------------------
+// Up to kFewTokens tokens, whose assignments nearly all go to experts of their own: products of
+// matrices with single vectors, bound by reading the weights once.  A wavefront takes whole rows
+// of them, 1 KiB per load instruction, and a lane multiplies its 16 bytes with the same piece of
+// the vector; no LDS on the way and nothing to wait for, so that all of a row's loads are in
+// flight.  (One token, 6 of 64 experts, H = 2048, F = 1408: the tiles' kernel has 132 workgroups
+// for that, each with one vector in 64 rows' place.)
+
+constexpr int kFewTokens = 4;
+constexpr int kFewSlots = 64;   // (one per lane)
+
+template <bool F32>
+__device__ __forceinline__ float dot16(mma_u32x4 a, mma_u32x4 b, float sum) {
+  if constexpr (F32) {
+    const mma_f32x4 x = __builtin_bit_cast(mma_f32x4, a), y = __builtin_bit_cast(mma_f32x4, b);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum = fmaf(x[i], y[i], sum);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      sum = fmaf(bf16_value(a[i] & 0xffffu), bf16_value(b[i] & 0xffffu), sum);
+      sum = fmaf(__builtin_bit_cast(float, a[i] & 0xffff0000u), __builtin_bit_cast(float, b[i] & 0xffff0000u), sum);
+    }
+  }
+  return sum;
+}
+__device__ __forceinline__ float lanes_sum(float x) {  // in all lanes, one fixed order
+#pragma unroll
+  for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d);
+  return x;
+}
+
+// sum[r] += row[r] times vector over the lane's pieces of chunks begin .. end - 1 (1 KiB each).
+template <bool F32, int ROWS, int BATCH>
+__device__ __forceinline__ void row_products(const unsigned char* const (&row)[ROWS], const unsigned char* vector, int bytes,
+                                             int begin, int end, int lane, float (&sum)[ROWS]) {
+  for (int c = begin; c < end; c += BATCH) {
+    mma_u32x4 x[BATCH], w[BATCH][ROWS];
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) {
+      const int at = (c + i) * 1024 + lane * 16;
+      const bool in = c + i < end && at < bytes;
+      const int from = in ? at : 0;
+      x[i] = *reinterpret_cast<const mma_u32x4*>(vector + from);
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r) {
+        w[i][r] = *reinterpret_cast<const mma_u32x4*>(row[r] + from);
+        if (!in) w[i][r] = mma_u32x4{0, 0, 0, 0};
+      }
+      if (!in) x[i] = mma_u32x4{0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i)
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r) sum[r] = dot16<F32>(w[i][r], x[i], sum[r]);
+  }
+}
+
+// The expert (of the call's) whose range of positions holds p, or -1; the same p in all lanes.
+__device__ __forceinline__ int expert_of(const ExpertTiles& t, int p) {
+  const unsigned long long has = __ballot(p >= t.lo && p < t.lo + t.cnt);
+  return has == 0 ? -1 : __builtin_ctzll(has);
+}
+
+// blockIdx.x: the position; blockIdx.y: 4 wavefronts x kFewUp columns of act.
+constexpr int kFewUp = 2;
+template <bool F32>
+__global__ __launch_bounds__(256) void experts_up_few_kernel(ExpertArgs a) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int p = blockIdx.x, f0 = (blockIdx.y * 4 + wave) * kFewUp;
+  ExpertTiles tiles;
+  tiles.init(a, lane);
+  const int e = expert_of(tiles, p);
+  if (e < 0 || f0 >= a.F) return;
+  const int t = a.permutation != nullptr ? min(max(a.permutation[p], 0), a.slots - 1) / a.k : p;
+  const unsigned char* row[2 * kFewUp];
+#pragma unroll
+  for (int i = 0; i < kFewUp; ++i) {
+    row[i] = a.w + ((size_t)e * 2 * a.F + min(f0 + i, a.F - 1)) * a.K;
+    row[kFewUp + i] = row[i] + (size_t)a.F * a.K;
+  }
+  float sum[2 * kFewUp] = {};
+  row_products<F32, 2 * kFewUp, 4>(row, a.x + (size_t)t * a.K, a.K, 0, (a.K + 1023) >> 10, lane, sum);
+#pragma unroll
+  for (int i = 0; i < kFewUp; ++i) {
+    const float y = silu<F32>(lanes_sum(sum[i])) * lanes_sum(sum[kFewUp + i]);
+    if (lane == 0 && f0 + i < a.F) {
+      if constexpr (F32) static_cast<float*>(a.out)[(size_t)p * a.F + f0 + i] = y;
+      else static_cast<unsigned short*>(a.out)[(size_t)p * a.F + f0 + i] = (unsigned short)bf16_bits(y);
+    }
+  }
+}
+
+// kFewRows rows of out (columns, for the caller) per workgroup.  Its wavefronts take the slots
+// in turn, and where there are fewer slots than wavefronts, parts of the rows as well; what they
+// find waits in LDS for its place in the sums, which run in slot order.
+constexpr int kFewRows = 8, kFewWaves = 8;
+template <bool F32>
+__global__ __launch_bounds__(64 * kFewWaves) void experts_down_few_kernel(ExpertArgs a, const int32_t* ids, int first,
+                                                                          const void* base, void* out, int T) {
+  __shared__ float found[kFewSlots * kFewRows];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int h0 = blockIdx.x * kFewRows;
+  ExpertTiles tiles;
+  tiles.init(a, lane);
+  // the slot at this lane's position (positions and slots: one per lane)
+  const int at = lane < a.slots ? (a.permutation != nullptr ? a.permutation[lane] : lane) : -1;
+  const int parts = a.slots <= kFewWaves / 4 ? 4 : a.slots <= kFewWaves / 2 ? 2 : 1;
+  const int chunks = (a.K + 1023) >> 10;
+  auto mine = [&](int slot) { return ids == nullptr || (unsigned)(ids[slot] - first) < (unsigned)a.E; };
+  for (int u = wave; u < a.slots * parts; u += kFewWaves) {
+    const int slot = u / parts, part = u - slot * parts;
+    const unsigned long long where = __ballot(at == slot);
+    const int p = where == 0 ? -1 : __builtin_ctzll(where);
+    const int e = p < 0 ? -1 : expert_of(tiles, p);
+    float sum[kFewRows] = {};
+    if (e >= 0 && mine(slot)) {
+      const unsigned char* row[kFewRows];
+#pragma unroll
+      for (int r = 0; r < kFewRows; ++r) row[r] = a.w + ((size_t)e * a.H + min(h0 + r, a.H - 1)) * a.K;
+      row_products<F32, kFewRows, 3>(row, a.x + (size_t)p * a.K, a.K, chunks * part / parts, chunks * (part + 1) / parts,
+                                     lane, sum);
+    }
+#pragma unroll
+    for (int r = 0; r < kFewRows; ++r) {
+      const float s = lanes_sum(sum[r]);
+      if (lane == 0) found[u * kFewRows + r] = s;
+    }
+  }
+  __syncthreads();
+  const int r = threadIdx.x % kFewRows, t = threadIdx.x / kFewRows, h = h0 + r;
+  if (t >= T || h >= a.H) return;
+  float y = 0.0f;
+  if (base != nullptr)
+    y = F32 ? static_cast<const float*>(base)[(size_t)t * a.H + h]
+            : bf16_value(static_cast<const unsigned short*>(base)[(size_t)t * a.H + h]);
+  for (int slot = t * a.k; slot < (t + 1) * a.k; ++slot) {
+    if (!mine(slot)) continue;
+    float z = 0.0f;
+    for (int part = 0; part < parts; ++part) z += found[(slot * parts + part) * kFewRows + r];
+    y += z * (a.weights != nullptr ? a.weights[slot] : 1.0f);
+  }
+  if constexpr (F32) static_cast<float*>(out)[(size_t)t * a.H + h] = y;
+  else static_cast<unsigned short*>(out)[(size_t)t * a.H + h] = (unsigned short)bf16_bits(y);
+}
+
 // out[t,:] = base[t,:] + the products of the token's slots that the call's experts hold, in
-// slot order.  One thread per four columns.
+// slot order.  One thread per four columns; the rows of four slots are under way at a time.
 template <bool F32>
 __global__ __launch_bounds__(256) void experts_combine_kernel(const float* z, const int32_t* ids, const void* base,
                                                               void* out, int T, int H, int k, int first, int E) {
@@ -202,33 +363,72 @@ __global__ __launch_bounds__(256) void experts_combine_kernel(const float* z, co
     const int h = (int)(i - t * quads) * 4;
     mma_f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
     if (base != nullptr) y = load4<F32>(base, t * H + h);
-    for (int j = 0; j < k; ++j) {
-      const size_t slot = t * k + j;
-      if (ids == nullptr || (unsigned)(ids[slot] - first) < (unsigned)E)
-        y += *reinterpret_cast<const mma_f32x4*>(z + slot * H + h);
+    for (int j = 0; j < k; j += 4) {
+      mma_f32x4 row[4];
+      int id[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) id[u] = ids == nullptr ? first : j + u < k ? ids[t * k + j + u] : -1;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        row[u] = mma_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        if (j + u < k && (unsigned)(id[u] - first) < (unsigned)E)
+          row[u] = __builtin_nontemporal_load(reinterpret_cast<const mma_f32x4*>(z + (t * k + j + u) * H + h));
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) y += row[u];
     }
     store4<F32>(out, t * H + h, y);
   }
 }
 
 constexpr int kGridMost = 1 << 20;
-constexpr int kLdsOfCu = 160 << 10;
 
-template <bool F32, bool UP, class TL>
-static hipError_t launch_experts(const ExpertArgs& a, hipStream_t s) {
-  static LdsAttr attr;
-  constexpr int kLds = TL::kLdsBytes + TL::BM * 12;  // the ring, and the table of the tile's rows
-  const void* fn = reinterpret_cast<const void*>(&experts_kernel<F32, UP, TL>);
-  hipError_t err = allow_dynamic_lds(fn, kLds, attr);
-  if (err != hipSuccess) return err;
+template <class TL>
+constexpr int lds_of() { return TL::kLdsBytes + TL::BM * 12; }  // the ring, and the table of the tile's rows
+template <class TL, bool UP>
+static long long grid_of(const ExpertArgs& a) {
   // (every expert with rows has at most one tile that is not full, and every tile a row)
   const long long mt = min((long long)a.slots, (long long)a.slots / TL::BM + min(a.E, a.slots));
   const int cols = UP ? TL::BN / 2 : TL::BN;
-  const long long grid = mt * (((UP ? a.F : a.H) + cols - 1) / cols);
-  const long long most = kLds > kLdsOfCu / 2 ? compute_units() : kGridMost;
-  hipLaunchKernelGGL((experts_kernel<F32, UP, TL>), dim3((unsigned)min(grid, most)),
-                     dim3(TL::kThreads), kLds, s, a);
+  return mt * (((UP ? a.F : a.H) + cols - 1) / cols);
+}
+
+template <bool F32, bool UP, class TL, bool MANY>
+static hipError_t launch_experts(const ExpertArgs& a, int rows, long long most, hipStream_t s) {
+  static LdsAttr attr;
+  const void* fn = reinterpret_cast<const void*>(&experts_kernel<F32, UP, TL, MANY>);
+  hipError_t err = allow_dynamic_lds(fn, lds_of<TL>(), attr);
+  if (err != hipSuccess) return err;
+  const unsigned grid = (unsigned)min(grid_of<TL, UP>(a), most);
+  hipLaunchKernelGGL((experts_kernel<F32, UP, TL, MANY>), dim3(grid), dim3(TL::kThreads), lds_of<TL>(), s, a, rows);
   return hipGetLastError();
+}
+
+// Which tiles.  bf16, by the rows per expert (us for H = 2048, F = 1408, 64 experts; tiles of
+// 64 x 128, 128 x 128 and 256 x 256):
+//   up:    48 rows on average 167, 182, -;   192 rows 304, 248, 230;   384 rows 514, 390, 327
+//   down:  48 rows 102, 110, -;              192 rows 198, 162, 166;   384 rows 338, 274, 240
+// The host knows the rows per expert if they were even, an upper bound where the call's experts are a
+// share of the layer's: only above kSomeRows are both of the larger tiles launched, with kManyRows
+// between them.  fp32 is bound by its matrix instructions (a sixteenth of the rate) as soon as there
+// are tiles for all compute units; before that, small tiles are more of them (333 tokens, 33
+// experts, 516 x 212: 30 us with tiles of 64 x 128, 20 with 32 x 64; 4000 tokens, 8 experts,
+// 1024 x 1024: 333 and 391).
+constexpr int kSomeRows = 96, kManyRows = 160;
+template <bool F32, bool UP>
+static hipError_t launch_products(const ExpertArgs& a, hipStream_t s) {
+  using LOW = Tile<F32, 64, 128, 2, 2, 3>;
+  if constexpr (F32) {
+    if (grid_of<LOW, UP>(a) < compute_units())
+      return launch_experts<F32, UP, Tile<F32, 32, 64, 2, 2, 6>, false>(a, 0, kGridMost, s);
+  } else if (a.slots >= (long long)kSomeRows * a.E) {
+    if (a.slots >= kManyRows) {
+      const hipError_t err = launch_experts<F32, UP, Tile<F32, 256, 256, 2, 4, 2>, true>(a, kManyRows, compute_units(), s);
+      if (err != hipSuccess) return err;
+    }
+    return launch_experts<F32, UP, Tile<F32, 128, 128, 2, 2, 2>, false>(a, kManyRows, 4 * compute_units(), s);
+  }
+  return launch_experts<F32, UP, LOW, false>(a, 0, kGridMost, s);
 }
 
 static int check_experts(int32_t T, int32_t H, int32_t F, int32_t E, const laser_experts_params_t* p) {
@@ -242,6 +442,9 @@ static int check_experts(int32_t T, int32_t H, int32_t F, int32_t E, const laser
   if (H % whole != 0 || F % whole != 0) return LASER_E_ALIGN;
   return LASER_OK;
 }
+
+// (F: a dimension of the grid)
+static bool are_few(int T, int slots, int F) { return T <= kFewTokens && slots <= kFewSlots && F <= 1 << 18; }
 
 static bool misaligned(const void* p) { return ((uintptr_t)p & 15) != 0; }
 
@@ -282,9 +485,15 @@ extern "C" int laser_experts_up(const void* hidden, const void* w_up, int32_t T,
   a.H = H;
   clear_stale_error();
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  const hipError_t err = f32 ? launch_experts<true, true, Tile<true, 64, 128, 1, 4, 3>>(a, s)
-                         : a.slots >= 128 * a.E ? launch_experts<false, true, Tile<false, 256, 256, 2, 4, 2>>(a, s)
-                             : launch_experts<false, true, Tile<false, 64, 128, 1, 4, 3>>(a, s);
+  if (are_few(T, a.slots, F)) {
+    const dim3 grid(a.slots, (F + 4 * kFewUp - 1) / (4 * kFewUp));
+    if (f32)
+      hipLaunchKernelGGL((experts_up_few_kernel<true>), grid, dim3(256), 0, s, a);
+    else
+      hipLaunchKernelGGL((experts_up_few_kernel<false>), grid, dim3(256), 0, s, a);
+    return hipGetLastError() == hipSuccess ? LASER_OK : LASER_E_LAUNCH;
+  }
+  const hipError_t err = f32 ? launch_products<true, true>(a, s) : launch_products<false, true>(a, s);
   return err == hipSuccess ? LASER_OK : LASER_E_LAUNCH;
 }
 
@@ -324,9 +533,17 @@ extern "C" int laser_experts_down(const void* act, const void* w_down, int32_t T
   a.H = H;
   clear_stale_error();
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  const hipError_t err = f32 ? launch_experts<true, false, Tile<true, 64, 128, 1, 4, 3>>(a, s)
-                         : a.slots >= 128 * a.E ? launch_experts<false, false, Tile<false, 256, 256, 2, 4, 2>>(a, s)
-                             : launch_experts<false, false, Tile<false, 64, 128, 1, 4, 3>>(a, s);
+  if (are_few(T, a.slots, F)) {
+    const dim3 grid((H + kFewRows - 1) / kFewRows);
+    if (f32)
+      hipLaunchKernelGGL((experts_down_few_kernel<true>), grid, dim3(64 * kFewWaves), 0, s, a, expert_ids,
+                         params->first_expert, base, out, T);
+    else
+      hipLaunchKernelGGL((experts_down_few_kernel<false>), grid, dim3(64 * kFewWaves), 0, s, a, expert_ids,
+                         params->first_expert, base, out, T);
+    return hipGetLastError() == hipSuccess ? LASER_OK : LASER_E_LAUNCH;
+  }
+  const hipError_t err = f32 ? launch_products<true, false>(a, s) : launch_products<false, false>(a, s);
   if (err != hipSuccess) return LASER_E_LAUNCH;
   const size_t quads = (size_t)T * (H / 4);
   const unsigned grid = (unsigned)min((quads + 255) / 256, (size_t)1 << 16);

@@ -222,7 +222,7 @@ struct Tile {
           const int r = (g + kAhead) % kGroups;
           t[r % MB] = token_block(behind < 0 ? slot : slot ^ kStage, r / MB, r % MB);
         }
-        if (g >= 1 && g <= NB) w[1][g - 1] = weight_block(slot, 1, g - 1);
+        if (g < NB) w[1][g] = weight_block(slot, 1, g);
         if (next && behind >= 0) {
 #pragma unroll
           for (int n = 0; n < NB; ++n)
@@ -241,7 +241,7 @@ struct Tile {
       }
       slot ^= kStage;
     };
-    static_assert((kStage & (kStage - 1)) == 0 && NB < MB, "slots that differ in one bit; weights of half a step read within it");
+    static_assert((kStage & (kStage - 1)) == 0 && NB <= MB, "slots that differ in one bit; weights of half a step read within it");
     if (steps > 1)
       asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kLoads) : "memory");
     else
@@ -272,7 +272,7 @@ __device__ __forceinline__ void store_tile(unsigned lds, int wave, int lane, VAL
   constexpr int kFit = kBytes / (16 * kRow);
   constexpr int kPass = kFit < TL::MB ? kFit : TL::MB;             // token blocks at a time
   constexpr int kPieces = kRow / 16, kRows = 64 / kPieces;         // pieces of a row; rows per store instruction
-  static_assert(kPass >= 1 && kPass * 16 % kRows == 0 && kPieces <= 16 && (kPieces & (kPieces - 1)) == 0, "whole instructions");
+  static_assert(kPass >= 1 && kPieces <= 16 && (kPieces & (kPieces - 1)) == 0, "whole instructions");
   const unsigned mine = lds + wave * kBytes;
   const int tok = lane & 15, quad = lane >> 4;
   constexpr int kTurn = kPieces - 1;  // (pieces are turned by the row, against bank conflicts)
@@ -294,14 +294,14 @@ __device__ __forceinline__ void store_tile(unsigned lds, int wave, int lane, VAL
         }
       }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    constexpr int kStores = kPass * 16 / kRows;
+    constexpr int kStores = (kPass * 16 + kRows - 1) / kRows;
     mma_u32x4 d[kStores];
     mma_u32x4* to[kStores];
 #pragma unroll
     for (int i = 0; i < kStores; ++i) {
       const int r = i * kRows + lane / kPieces, c = lane % kPieces;
-      to[i] = m0 + r / 16 < TL::MB ? static_cast<mma_u32x4*>(place(TL::block_row(wave, m0 + r / 16) + r % 16, c * (F32 ? 4 : 8))) : nullptr;
-      d[i] = read_lds(mine + r * kRow + (c ^ (r & kTurn)) * 16);
+      to[i] = r < kPass * 16 && m0 + r / 16 < TL::MB ? static_cast<mma_u32x4*>(place(TL::block_row(wave, m0 + r / 16) + r % 16, c * (F32 ? 4 : 8))) : nullptr;
+      d[i] = read_lds(mine + min(r, kPass * 16 - 1) * kRow + (c ^ (r & kTurn)) * 16);
     }
 #pragma unroll
     for (int i = 0; i < kStores; ++i)
