@@ -14,6 +14,8 @@
 
 namespace laser {
 
+constexpr int kThinSlices = 8;
+
 struct ProjectArgs {
   const unsigned char* x;  // [T, K]
   const unsigned char* w;  // [N, K]
@@ -45,49 +47,59 @@ __device__ __forceinline__ int requests_begun(const ProjectArgs& a, int t, int l
   return lo + __popcll(__ballot(lane < len && a.request_offsets[lo + min(lane, max(len - 1, 0))] <= t));
 }
 
-// The adapter of row t0 + lane % 16, or -1.
+// The adapter of row t0 + lane % 16, or -1.  A row belongs to the last request that begins at or
+// before it, if that one has not ended.
 __device__ __forceinline__ int adapter_of_row(const ProjectArgs& a, int t0, int lane) {
-  if (a.requests == 0) return -1;
   const int t = t0 + (lane & 15);
-  const int first = requests_begun(a, t0, lane);
-  // the requests that begin behind t0: 64 at a time
-  int begun = first;
-  for (int at = first; at < a.requests; at += 64) {
-    const int start = at + lane < a.requests ? a.request_offsets[at + lane] : 0x7fffffff;
-    if (__ballot(start <= t0 + 15) == 0) break;
+  // 64 requests at a time, from the one that row t0 may belong to
+  int m = -1;
+  for (int at = a.requests <= 64 ? 0 : max(requests_begun(a, t0, lane) - 1, 0); at < a.requests; at += 64) {
+    const bool is = at + lane < a.requests;
+    const int q = is ? at + lane : 0;
+    const int begin = a.request_offsets[q], end = a.request_offsets[q + 1], adapter = a.request_adapters[q];
+    int n = 0;  // of these, how many begin at or before this lane's row
 #pragma unroll
-    for (int i = 1; i < 16; ++i) {
-      const int n = __popcll(__ballot(start <= t0 + i));
-      if ((lane & 15) == i) begun += n;
+    for (int i = 0; i < 16; ++i) {
+      const int c = __popcll(__ballot(is && begin <= t0 + i));
+      if ((lane & 15) == i) n = c;
     }
+    const int last = max(n - 1, 0), its_end = __shfl(end, last), its_adapter = __shfl(adapter, last);
+    if (n > 0) m = t < its_end ? its_adapter : -1;
+    if (__ballot(is && begin <= t0 + 15) != ~0ull) break;
   }
-  if (begun == 0 || t >= a.T || t >= a.request_offsets[begun]) return -1;
-  const int m = a.request_adapters[begun - 1];
-  return (unsigned)m < (unsigned)a.M ? m : -1;
+  return t < a.T && (unsigned)m < (unsigned)a.M ? m : -1;
 }
 
 // acc[b] += rows (16 b + lane % 16) of `rows` times the 16 token rows, columns of k-steps (64
-// bytes) from `begin` to `end`.  Operands go memory -> registers, four steps in flight.
+// bytes) from `begin` to `end`.  Operands go memory -> registers, a batch of steps at a time.
+// Pieces behind the rows' end are zero in both operands: what lies there may be anything.
+constexpr int kThinBatch = 4;
+__device__ __forceinline__ mma_u32x4 thin_piece(const unsigned char* row, int bytes, int k, int end, int lane) {
+  const int at = k * 64 + (lane >> 4) * 16;
+  const bool in = k < end && at < bytes;
+  const mma_u32x4 x = *reinterpret_cast<const mma_u32x4*>(row + (in ? at : 0));
+  return in ? x : mma_u32x4{0, 0, 0, 0};
+}
+// The first batch of the token rows, for a caller that has something else to wait for meanwhile.
+struct ThinTokens {
+  mma_u32x4 t[kThinBatch];
+  __device__ ThinTokens(const unsigned char* tokens, int bytes, int begin, int end, int lane) {
+#pragma unroll
+    for (int i = 0; i < kThinBatch; ++i) t[i] = thin_piece(tokens, bytes, begin + i, end, lane);
+  }
+};
 template <bool F32, int B>
-__device__ __forceinline__ void thin_product(const unsigned char* tokens, const unsigned char* const (&rows)[B], int bytes,
-                                             int begin, int end, int lane, mma_f32x4 (&acc)[B]) {
-  const int own = (lane >> 4) * 16;
-  constexpr int kBatch = B <= 2 ? 4 : 2;
+__device__ __forceinline__ void thin_product(const ThinTokens& head, const unsigned char* tokens,
+                                             const unsigned char* const (&rows)[B], int bytes, int begin, int end, int lane,
+                                             mma_f32x4 (&acc)[B]) {
+  constexpr int kBatch = B <= 2 ? kThinBatch : 2;
   for (int k = begin; k < end; k += kBatch) {
     mma_u32x4 t[kBatch], r[kBatch][B];
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
-      const int at = (k + i) * 64 + own;
-      const bool in = k + i < end && at < bytes;
-      const int from = in ? at : 0;
-      t[i] = *reinterpret_cast<const mma_u32x4*>(tokens + from);
+      t[i] = k == begin ? head.t[i] : thin_piece(tokens, bytes, k + i, end, lane);
 #pragma unroll
-      for (int b = 0; b < B; ++b) r[i][b] = *reinterpret_cast<const mma_u32x4*>(rows[b] + from);
-      if (!in) {  // both operands: what lies there may be anything
-        t[i] = mma_u32x4{0, 0, 0, 0};
-#pragma unroll
-        for (int b = 0; b < B; ++b) r[i][b] = mma_u32x4{0, 0, 0, 0};
-      }
+      for (int b = 0; b < B; ++b) r[i][b] = thin_piece(rows[b], bytes, k + i, end, lane);
     }
 #pragma unroll
     for (int i = 0; i < kBatch; ++i)
@@ -132,11 +144,12 @@ __global__ __launch_bounds__(256) void adapter_inner_kernel(ProjectArgs a) {
   const int steps = (a.K + 63) >> 6, parts = 4 * (THIN ? a.slices : 1), own = (THIN ? 4 * (int)blockIdx.z : 0) + wave;
   const int begin = (int)((long long)steps * own / parts), end = (int)((long long)steps * (own + 1) / parts);
   const unsigned char* const tokens = a.x + (size_t)min(t, a.T - 1) * a.K;
+  const ThinTokens head(tokens, a.K, begin, end, lane);
   if (THIN && (int)blockIdx.y >= a.lanes) {
     const int n0 = (blockIdx.y - a.lanes) * 16;
     const unsigned char* rows[1] = {a.w + (size_t)min(n0 + (lane & 15), a.N - 1) * a.K};
     mma_f32x4 acc[1] = {mma_f32x4{0.0f, 0.0f, 0.0f, 0.0f}};
-    thin_product<F32, 1>(tokens, rows, a.K, begin, end, lane, acc);
+    thin_product<F32, 1>(head, tokens, rows, a.K, begin, end, lane, acc);
     join_wavefronts<1>(acc, part, wave, lane, [&](int, mma_f32x4 sum) {
       if (t >= a.T) return;
 #pragma unroll
@@ -161,7 +174,7 @@ __global__ __launch_bounds__(256) void adapter_inner_kernel(ProjectArgs a) {
     mma_f32x4 acc[B];
 #pragma unroll
     for (int b = 0; b < B; ++b) acc[b] = mma_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    thin_product<F32, B>(tokens, rows, a.K, begin, end, lane, acc);
+    thin_product<F32, B>(head, tokens, rows, a.K, begin, end, lane, acc);
     const float scale = THIN || a.scales == nullptr ? 1.0f : a.scales[ad];
     join_wavefronts<B>(acc, part, wave, lane, [&](int b, mma_f32x4 sum) {
       const int r = b * 16 + 4 * (lane >> 4);
@@ -181,32 +194,50 @@ __global__ __launch_bounds__(256) void adapter_inner_kernel(ProjectArgs a) {
   }
 }
 
-// Thin calls, second launch: one workgroup per row and 256 columns.
+// Thin calls, second launch: one workgroup per row and as many columns as it has threads.  All
+// that does not wait for another load is under way at once: the slices, the first 16 values of
+// the column's row of U.
 template <bool F32, bool OUT32>
 __global__ __launch_bounds__(256) void adapter_join_kernel(ProjectArgs a) {
   __shared__ float v[LASER_MAX_RANK];
-  const int t = blockIdx.x, n = blockIdx.y * 256 + threadIdx.x;
+  const int t = blockIdx.x, n = blockIdx.y * blockDim.x + threadIdx.x, column = min(n, a.N - 1);
   const int m = a.adapter[t];
-  if (m >= 0 && (int)threadIdx.x < a.R) {
-    float sum = 0.0f;
-    for (int s = 0; s < a.slices; ++s) sum += static_cast<const float*>(a.inner)[((size_t)s * a.T + t) * a.R + threadIdx.x];
-    v[threadIdx.x] = sum * (a.scales != nullptr ? a.scales[m] : 1.0f);
-  }
-  float y = 0.0f;
-  if (n < a.N)
-    for (int s = 0; s < a.slices; ++s) y += a.shared[((size_t)s * a.T + t) * a.N + n];
-  __syncthreads();
-  if (n >= a.N) return;
-  if (m >= 0) {
-    const size_t row = ((size_t)m * a.N + n) * a.R;
-    float d = 0.0f;
-    for (int r = 0; r < a.R; r += 4) {
-      const mma_f32x4 u = load4<F32>(a.a_up, row + r);
+  float part[kThinSlices];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) d = fmaf(u[i], v[r + i], d);
+  for (int s = 0; s < kThinSlices; ++s)
+    part[s] = s < a.slices ? a.shared[((size_t)s * a.T + t) * a.N + column] : 0.0f;
+  float y = 0.0f;
+#pragma unroll
+  for (int s = 0; s < kThinSlices; ++s) y += part[s];
+  if (m >= 0) {  // (the same for the whole workgroup)
+    const size_t row = ((size_t)m * a.N + column) * a.R;
+    mma_f32x4 u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[i] = load4<F32>(a.a_up, row + min(4 * i, a.R - 4));
+    for (int r = threadIdx.x; r < a.R; r += blockDim.x) {
+#pragma unroll
+      for (int s = 0; s < kThinSlices; ++s)
+        part[s] = s < a.slices ? static_cast<const float*>(a.inner)[((size_t)s * a.T + t) * a.R + r] : 0.0f;
+      float sum = 0.0f;
+#pragma unroll
+      for (int s = 0; s < kThinSlices; ++s) sum += part[s];
+      v[r] = sum * (a.scales != nullptr ? a.scales[m] : 1.0f);
+    }
+    __syncthreads();
+    float d = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (4 * j < a.R)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) d = fmaf(u[j][i], v[4 * j + i], d);
+    for (int r = 16; r < a.R; r += 4) {
+      const mma_f32x4 more = load4<F32>(a.a_up, row + r);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) d = fmaf(more[i], v[r + i], d);
     }
     y += d;
   }
+  if (n >= a.N) return;
   const size_t at = (size_t)t * a.N + n;
   if constexpr (OUT32) static_cast<float*>(a.out)[at] = y;
   else static_cast<unsigned short*>(a.out)[at] = (unsigned short)bf16_bits(y);
@@ -275,6 +306,36 @@ __device__ __forceinline__ void add_adapters(const ProjectArgs& a, int t0, int n
   }
 }
 
+// A wavefront's results (NC blocks of columns from n0 on) to out: whole 16-byte pieces where the
+// rows of out consist of them, values one by one where they do not.
+template <bool OUT32, class TL, int NC>
+__device__ __forceinline__ void store_columns(const ProjectArgs& a, unsigned lds, int wave, int lane, int t0, int rows, int n0,
+                                              mma_f32x4 (&y)[NC][TL::MB]) {
+  constexpr int kSize = OUT32 ? 4 : 2;
+  if (a.N % (16 / kSize) == 0) {
+    store_tile<OUT32, TL, NC>(
+        lds, wave, lane, [&](int n, int m) { return y[n][m]; },
+        [&](int r, int c) -> void* {
+          return r < rows && n0 + c < a.N ? static_cast<char*>(a.out) + ((size_t)(t0 + r) * a.N + n0 + c) * kSize : nullptr;
+        });
+    return;
+  }
+#pragma unroll
+  for (int m = 0; m < TL::MB; ++m) {
+    const int r = TL::block_row(wave, m) + (lane & 15);
+#pragma unroll
+    for (int n = 0; n < NC; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int c = n0 + n * 16 + 4 * (lane >> 4) + i;
+        if (r >= rows || c >= a.N) continue;
+        const size_t at = (size_t)(t0 + r) * a.N + c;
+        if constexpr (OUT32) static_cast<float*>(a.out)[at] = y[n][m][i];
+        else static_cast<unsigned short*>(a.out)[at] = (unsigned short)bf16_bits(y[n][m][i]);
+      }
+  }
+}
+
 template <bool F32, bool OUT32, class TL>
 __global__ __launch_bounds__(TL::kThreads) void project_kernel(ProjectArgs a) {
   extern __shared__ __align__(1024) unsigned char ring[];
@@ -308,36 +369,145 @@ __global__ __launch_bounds__(TL::kThreads) void project_kernel(ProjectArgs a) {
     int l = lane;
     asm volatile("" : "+v"(l));
     add_adapters<F32, TL>(a, t0, n0, blocks, wave, l, acc);
-    constexpr int kSize = OUT32 ? 4 : 2;
-    if (a.N % (16 / kSize) == 0) {
-      store_tile<OUT32, TL, NB>(
-          lds, wave, l, [&](int n, int m) { return acc[n][m]; },
-          [&](int r, int c) -> void* {
-            return r < rows && n0 + c < a.N ? static_cast<char*>(a.out) + ((size_t)(t0 + r) * a.N + n0 + c) * kSize : nullptr;
-          });
-    } else {
+    store_columns<OUT32, TL, NB>(a, lds, wave, l, t0, rows, n0, acc);
+    lds_barrier();  // (the ring is free again)
+  }
+}
+
+// Up to 64 columns (a gate) and adapters of rank up to 64: one launch that reads x once.  The
+// weight rows of a tile are W's and behind them 64 rows of inner matrices, of the first adapters
+// that its 64 rows have; each wavefront has 16 rows, all columns and their v, whose accumulator
+// layout (row 4 (lane / 16) + i) serves as the operand of the second product as it is: which
+// slot of a matrix instruction is which r is free, as long as U's rows are read the same way.
+// A tile with more adapters makes another pass over its rows for every 128 rows of them.
+// (16384 rows, H = 2048, 64 columns, rank 16: 25 us against 50 with a launch of its own for v, which
+// reads x a second time; bound by reading x, 13 us at the rate of a large copy.)
+constexpr int kNarrowColumns = 64, kNarrowRank = 64;
+template <bool F32, bool OUT32, int RB>  // RB: blocks of 16 that hold an adapter's rows
+__global__ __launch_bounds__(256) void project_narrow_kernel(ProjectArgs a) {
+  using TL = Tile<F32, 64, 128, 4, 1, 6>;
+  constexpr int kRoom = 4 / RB;  // adapters beside W, twice that without
+  extern __shared__ __align__(1024) unsigned char ring[];
+  int* const ids = reinterpret_cast<int*>(ring + TL::kLdsBytes);
+  const unsigned lds = (unsigned)(size_t)(lds_bytes)ring;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const TL tile(a.K, lds, wave, lane);
+  const int tok = lane & 15, quad = lane >> 4;
+  const int tiles = (a.T + 63) >> 6;
+  for (int v = blockIdx.x; v < tiles; v += gridDim.x) {
+    const int t0 = xcd_run(v, tiles) * 64, rows = min(a.T - t0, 64);
+    const int m = adapter_of_row(a, t0 + wave * 16, lane);
+    if (lane < 16) ids[wave * 16 + lane] = m;
+    lds_barrier();
+    const int id = ids[lane];  // of row t0 + lane
+    unsigned long long todo = __ballot(id >= 0);
+    const unsigned char* from[TL::kLoads];
+    const int piece = TL::piece(wave, lane) * 16;
+    mma_f32x4 y[4][1];  // the tile's results
+    for (bool first = true; first || todo != 0; first = false) {
+      // the adapters of this pass, in order; rows of inner matrices that are not needed repeat others
+      int held[2 * kRoom];
 #pragma unroll
-      for (int m = 0; m < MB; ++m) {
-        const int r = TL::block_row(wave, m) + (l & 15);
+      for (int q = 0; q < 2 * kRoom; ++q) {
+        held[q] = -1;
+        if (todo != 0 && (q < kRoom || !first)) {
+          held[q] = __builtin_amdgcn_readlane(id, __builtin_ctzll(todo));
+          todo &= ~__ballot(id == held[q]);
+        }
+      }
 #pragma unroll
-        for (int n = 0; n < NB; ++n)
+      for (int i = 0; i < TL::kLoads; ++i) {
+        const int r = TL::row(wave, lane, i), w = r - 64;  // (rows 0 .. 63 are tokens)
+        if (r < 64) {
+          from[i] = a.x + (size_t)min(t0 + r, a.T - 1) * a.K + piece;
+        } else if (first && w < 64) {
+          from[i] = a.w + (size_t)min(w, a.N - 1) * a.K + piece;
+        } else {
+          const int x = first ? w - 64 : w, which = x / (16 * RB);  // (the same for all lanes of a load instruction)
+          int ad = -1;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int c = n0 + n * 16 + 4 * (l >> 4) + i;
-            const size_t at = (size_t)(t0 + r) * a.N + c;
-            if (r >= rows || c >= a.N) continue;
-            if constexpr (OUT32) static_cast<float*>(a.out)[at] = acc[n][m][i];
-            else static_cast<unsigned short*>(a.out)[at] = (unsigned short)bf16_bits(acc[n][m][i]);
+          for (int q = 0; q < 2 * kRoom; ++q) ad = which == q ? held[q] : ad;
+          if (ad < 0) ad = held[0];
+          from[i] = (ad < 0 ? a.w : a.a_down + ((size_t)ad * a.R + min(x % (16 * RB), a.R - 1)) * a.K) + piece;
+        }
+      }
+      mma_f32x4 acc[8][1];
+#pragma unroll
+      for (int n = 0; n < 8; ++n) acc[n][0] = mma_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      tile.start(from);
+      tile.run(from, 1, acc);
+      if (first)
+#pragma unroll
+        for (int n = 0; n < 4; ++n) y[n][0] = acc[n][0];
+#pragma unroll
+      for (int q = 0; q < 2 * kRoom; ++q) {
+        if (held[q] < 0 || __ballot(m == held[q]) == 0) continue;
+        const bool mine = m == held[q];
+        const float scale = a.scales != nullptr ? a.scales[held[q]] : 1.0f;
+        mma_f32x4 d[4];
+#pragma unroll
+        for (int n = 0; n < 4; ++n) d[n] = mma_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int b = 0; b < RB; b += F32 ? 1 : 2) {
+          mma_f32x4 inner[2];  // blocks b and, bf16, b + 1
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int n = q * RB + min(b + h, RB - 1);
+            inner[h] = first ? acc[(4 + n) & 7][0] : acc[n & 7][0];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) inner[h][i] = mine && b + h < RB ? inner[h][i] * scale : 0.0f;
           }
+          const int r = 16 * b + 4 * quad;
+#pragma unroll
+          for (int n = 0; n < 4; ++n) {
+            const size_t row = ((size_t)held[q] * a.N + min(16 * n + tok, a.N - 1)) * a.R;
+            if constexpr (F32) {
+              mma_f32x4 u = {0.0f, 0.0f, 0.0f, 0.0f};
+              if (r < a.R) u = load4<true>(a.a_up, row + r);
+              const mma_f32x4 x = r < a.R ? inner[0] : mma_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+              d[n] = multiply<true>(__builtin_bit_cast(mma_u32x4, u), __builtin_bit_cast(mma_u32x4, x), d[n]);
+            } else {
+              const unsigned short* const up = reinterpret_cast<const unsigned short*>(a.a_up) + row;
+              mma_u32x4 u = {0, 0, 0, 0}, p[3];
+              if (r < a.R) {
+                const mma_u32x2 lo = *reinterpret_cast<const mma_u32x2*>(up + r);
+                u[0] = lo[0], u[1] = lo[1];
+              }
+              if (b + 1 < RB && r + 16 < a.R) {
+                const mma_u32x2 hi = *reinterpret_cast<const mma_u32x2*>(up + r + 16);
+                u[2] = hi[0], u[3] = hi[1];
+              }
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                const bool in = r + 16 * h < a.R;  // (rows past the rank repeat the last one: not used)
+                unsigned s[4][3];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) split3(in ? inner[h][i] : 0.0f, s[i]);
+#pragma unroll
+                for (int j = 0; j < 3; ++j) {
+                  p[j][2 * h] = s[0][j] | s[1][j] << 16;
+                  p[j][2 * h + 1] = s[2][j] | s[3][j] << 16;
+                }
+              }
+#pragma unroll
+              for (int j = 2; j >= 0; --j) d[n] = multiply<false>(u, p[j], d[n]);
+            }
+          }
+        }
+        // (not added to rows of other adapters: a zero times an infinity in u is no zero)
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) y[n][0][i] += mine ? d[n][i] : 0.0f;
       }
     }
-    lds_barrier();  // (the ring is free again)
+    store_columns<OUT32, TL, 4>(a, lds, wave, lane, t0, rows, 0, y);
+    lds_barrier();  // (the ring and the ids are free again)
   }
 }
 
 // ---- host ---------------------------------------------------------------------------
 
-constexpr int kThinSlices = 8;
 constexpr int kThinRows = 512, kThinValues = 1 << 16;
 static bool is_thin(int T, int N) { return T <= kThinRows && (long long)T * N <= kThinValues; }
 
@@ -395,6 +565,17 @@ static hipError_t launch_tiles(const ProjectArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <bool F32, bool OUT32, int RB>
+static hipError_t launch_narrow(const ProjectArgs& a, hipStream_t s) {
+  static LdsAttr attr;
+  constexpr int kLds = Tile<F32, 64, 128, 4, 1, 6>::kLdsBytes + 64 * 4;
+  const void* fn = reinterpret_cast<const void*>(&project_narrow_kernel<F32, OUT32, RB>);
+  hipError_t err = allow_dynamic_lds(fn, kLds, attr);
+  if (err != hipSuccess) return err;
+  hipLaunchKernelGGL((project_narrow_kernel<F32, OUT32, RB>), dim3(min((a.T + 63) / 64, 1 << 20)), dim3(256), kLds, s, a);
+  return hipGetLastError();
+}
+
 template <bool F32, bool OUT32>
 static hipError_t launch_project(ProjectArgs& a, hipStream_t s) {
   const int rows16 = (a.T + 15) / 16;
@@ -404,9 +585,14 @@ static hipError_t launch_project(ProjectArgs& a, hipStream_t s) {
     a.lanes = a.requests > 0 ? min(16, a.requests) : 1;
     hipError_t err = launch_inner<F32, true>(a, dim3(rows16, a.lanes + (a.N + 15) / 16, a.slices), s);
     if (err != hipSuccess) return err;
-    hipLaunchKernelGGL((adapter_join_kernel<F32, OUT32>), dim3(a.T, (a.N + 255) / 256), dim3(256), 0, s, a);
+    const int threads = a.N <= 64 ? 64 : a.N <= 128 ? 128 : 256;
+    hipLaunchKernelGGL((adapter_join_kernel<F32, OUT32>), dim3(a.T, (a.N + threads - 1) / threads), dim3(threads), 0, s, a);
     return hipGetLastError();
   }
+  if (a.N <= kNarrowColumns && a.R <= kNarrowRank)
+    return a.R <= 16   ? launch_narrow<F32, OUT32, 1>(a, s)
+           : a.R <= 32 ? launch_narrow<F32, OUT32, 2>(a, s)
+                       : launch_narrow<F32, OUT32, 4>(a, s);
   a.slices = 1;
   a.lanes = a.requests > 0 ? min(min(16, a.requests), max(1, 1024 / rows16)) : 1;
   hipError_t err = launch_inner<F32, false>(a, dim3(rows16, a.lanes, 1), s);

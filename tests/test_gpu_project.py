@@ -30,6 +30,8 @@ SHAPES = [
     (40, 64, 16, 8, 1, []),                         # no requests
     (513, 136, 24, 24, 700, [1] * 300 + [0, 0] * 100 + [3] * 71),   # hundreds of requests, many of them empty
     (600, 136, 130, 104, 5, [0] * 70 + [5] * 40 + [0] * 5000 + [400]),
+    (700, 264, 40, 64, 6, [1] * 70 + [5, 60, 65, 500]),              # many adapters in a tile of a gate
+    (1200, 136, 64, 48, 9, [400, 1, 1, 1, 797]),
     (4200, 200, 2061, 40, 6, [900, 20, 1, 2000, 1279]),              # the widest tiles, odd columns
     (4100, 72, 2560, 128, 3, [1024, 1, 3075]),
 ]
