@@ -99,8 +99,9 @@ struct Tile {
   static constexpr int kLoads = (BM + BN) / 8 / kWaves;       // load instructions of a wavefront per step
   static constexpr int kStage = (BM + BN) * kStepBytes;
   static constexpr int kLdsBytes = ST * kStage;
+  static constexpr int kStaging = ST == 2 ? kStage : kLdsBytes;  // what store_tile may use of it
   static_assert(kLoads * 8 * kWaves == BM + BN && kWaves % 2 == 0 && ST >= 2, "whole load instructions per wavefront");
-  static_assert((ST - 2) * kLoads < 64, "vmcnt counts to 63");
+  static_assert((ST - 1) * kLoads < 64, "vmcnt counts to 63");
 
   // Tile row that load i of this wavefront brings for this lane (tokens 0 .. BM - 1, then
   // weights), and the piece of that row: the same for all i, as kWaves is even.
@@ -108,15 +109,15 @@ struct Tile {
   __device__ static int piece(int wave, int lane) { return (lane & 7) ^ ((wave & 1) * 4 + (lane >> 4)); }
 
   // The product of one tile.  from[i]: where load i of this lane begins (row start + 16 *
-  // piece); `bytes`: length of the rows, a multiple of 16.  start() puts the first steps on
+  // piece + kStepBytes * turn); `bytes`: length of the rows, a multiple of 16.  start() puts the first steps on
   // their way to LDS, which nobody may be reading any more; run() does the rest and ends with
   // every wavefront through with its reads of LDS.
-  int steps;
+  int steps, bytes;
   bool in_last;    // whether this lane's piece of the last step is inside the rows
   unsigned put;    // where this wavefront's loads go in slot 0
   unsigned get_t, get_w;  // this lane's operands in slot 0, first half of the step
 
-  __device__ Tile(int bytes, unsigned lds, int wave, int lane) {
+  __device__ Tile(int bytes_, unsigned lds, int wave, int lane) : bytes(bytes_), turn(0), column(0) {
     steps = (bytes + kStepBytes - 1) / kStepBytes;
     in_last = piece(wave, lane) * 16 < bytes - (steps - 1) * kStepBytes;
     put = __builtin_amdgcn_readfirstlane(lds + wave * 8 * kStepBytes);
@@ -125,17 +126,34 @@ struct Tile {
     get_w = lds + (BM + wave / WM * (BN / WN)) * kStepBytes + get;
   }
 
+  // Which columns a tile begins with: rows whose length is a multiple of a step may be walked
+  // from any step on and around (`turn`).  Rows often lie a power of two apart, and then all tiles
+  // that are at the same step read from the same few memory channels.
+  int turn;    // step of the rows that is loaded first
+  int column;  // ... next
+  __device__ void turn_to(int which) {
+    turn = steps * kStepBytes == bytes ? which % steps : 0;
+    column = turn;
+  }
+  // bytes from this step of the rows to the next one loaded
+  __device__ int stride() {
+    const bool around = column == steps - 1;
+    column = around ? 0 : column + 1;
+    return around ? kStepBytes - steps * kStepBytes : kStepBytes;
+  }
+
   template <typename LAST>
-  __device__ void load(const unsigned char* (&from)[kLoads], LAST last, unsigned slot, int i) const {
+  __device__ void load(const unsigned char* (&from)[kLoads], LAST last, unsigned slot, int i, int by) const {
     const unsigned char* p = from[i];
-    from[i] += kStepBytes;
+    from[i] += by;
     if (last) p = in_last ? p : reinterpret_cast<const unsigned char*>(zero_piece);
     load_to_lds(p, put + slot + i * kWaves * 8 * kStepBytes);
   }
   template <typename LAST>
-  __device__ void load_all(const unsigned char* (&from)[kLoads], LAST last, unsigned slot) const {
+  __device__ void load_all(const unsigned char* (&from)[kLoads], LAST last, unsigned slot) {
+    const int by = stride();
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) load(from, last, slot, i);
+    for (int i = 0; i < kLoads; ++i) load(from, last, slot, i, by);
   }
   // Blocks of 16 tokens go to the WM wavefronts of a column in turn, so that a tile with few
   // rows is work for all of them: row of token block m, and how many blocks have rows at all.
@@ -150,21 +168,20 @@ struct Tile {
     return read_lds(((get_w + slot) ^ (s * 64)) + n * 16 * kStepBytes);
   }
 
-  __device__ void start(const unsigned char* (&from)[kLoads]) const {
-    constexpr int kAhead = ST == 2 ? 2 : ST - 1;
+  __device__ void start(const unsigned char* (&from)[kLoads]) {
 #pragma unroll
-    for (int s = 0; s < kAhead; ++s)
+    for (int s = 0; s < ST; ++s)
       if (s < steps) load_all(from, s == steps - 1, s * kStage);
   }
 
   // start() in two parts: between them only the first half of the ring is being filled
-  __device__ void start_first(const unsigned char* (&from)[kLoads]) const { load_all(from, steps == 1, 0); }
-  __device__ void start_second(const unsigned char* (&from)[kLoads]) const {
+  __device__ void start_first(const unsigned char* (&from)[kLoads]) { load_all(from, steps == 1, 0); }
+  __device__ void start_second(const unsigned char* (&from)[kLoads]) {
     if (steps > 1) load_all(from, steps == 2, kStage);
   }
 
   // `blocks`: this wavefront's token blocks that have rows; the others' products are left out
-  __device__ void run(const unsigned char* (&from)[kLoads], int blocks, mma_f32x4 (&acc)[NB][MB]) const {
+  __device__ void run(const unsigned char* (&from)[kLoads], int blocks, mma_f32x4 (&acc)[NB][MB]) {
     if constexpr (ST == 2)
       run_interleaved(from, blocks, acc);
     else
@@ -172,31 +189,58 @@ struct Tile {
     lds_barrier();
   }
 
-  __device__ void run_ring(const unsigned char* (&from)[kLoads], int blocks, mma_f32x4 (&acc)[NB][MB]) const {
+  // ST slots.  A step's operands are read while the step before is multiplied; with that its slot is
+  // free, and ST - 1 steps are on their way.
+  __device__ void run_ring(const unsigned char* (&from)[kLoads], int blocks, mma_f32x4 (&acc)[NB][MB]) {
+    mma_u32x4 w[2][2][NB], t[2][2][MB];  // [step % 2][half]
     unsigned slot = 0;
-    for (int step = 0; step < steps; ++step) {
-      // this wavefront's loads of the step are there, and its reads of the step before
-      // are done, for which the slot that is loaded next was waiting
-      if (step + ST - 1 <= steps)
+    auto read = [&](int at) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+#pragma unroll
+        for (int n = 0; n < NB; ++n) w[at][s][n] = weight_block(slot, s, n);
+#pragma unroll
+        for (int m = 0; m < MB; ++m)
+          if (m < blocks) t[at][s][m] = token_block(slot, s, m);
+      }
+      __builtin_amdgcn_sched_barrier(0);  // (the compiler would put the reads behind the products)
+    };
+    auto products = [&](int at) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int m = 0; m < MB; ++m)
+          if (m < blocks)
+#pragma unroll
+            for (int n = 0; n < NB; ++n) acc[n][m] = multiply<F32>(w[at][s][n], t[at][s][m], acc[n][m]);
+    };
+    // step + 1 is there, and everybody has read `step`, whose slot is loaded again
+    auto hand_over = [&](int step) {
+      if (step + ST <= steps)
         asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((ST - 2) * kLoads) : "memory");
       else
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-      if (step + ST - 1 < steps)
-        load_all(from, step + ST == steps, slot == 0 ? (ST - 1) * kStage : slot - kStage);
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        mma_u32x4 w[NB], t[MB];
-#pragma unroll
-        for (int n = 0; n < NB; ++n) w[n] = weight_block(slot, s, n);
-#pragma unroll
-        for (int m = 0; m < MB; ++m)
-          if (m < blocks) {
-            t[m] = token_block(slot, s, m);
-#pragma unroll
-            for (int n = 0; n < NB; ++n) acc[n][m] = multiply<F32>(w[n], t[m], acc[n][m]);
-          }
-      }
+      if (step + ST < steps) load_all(from, step + ST == steps - 1, slot);
       slot = slot == (ST - 1) * kStage ? 0 : slot + kStage;
+    };
+    if (steps >= ST)
+      asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((ST - 1) * kLoads) : "memory");
+    else
+      asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+    read(0);
+    for (int step = 0; step < steps; step += 2) {
+      if (step + 1 < steps) {
+        hand_over(step);
+        read(1);
+      }
+      products(0);
+      if (step + 1 < steps) {
+        if (step + 2 < steps) {
+          hand_over(step + 1);
+          read(0);
+        }
+        products(1);
+      }
     }
   }
 
@@ -209,11 +253,12 @@ struct Tile {
   // 8192 x 4096 in bf16 took 462 us instead of 387, with one more memory round trip exposed per
   // step; the matrix instructions alone, on the same operands, take 345: the card lowers its
   // clock under them.  Loads in bursts of two per group: 404; the barrier two groups later: 394.)
-  __device__ void run_interleaved(const unsigned char* (&from)[kLoads], int blocks, mma_f32x4 (&acc)[NB][MB]) const {
+  __device__ void run_interleaved(const unsigned char* (&from)[kLoads], int blocks, mma_f32x4 (&acc)[NB][MB]) {
     constexpr int kGroups = 2 * MB, kAhead = MB - 1;
     mma_u32x4 w[2][NB], t[MB];
     unsigned slot = 0;
     auto step = [&](auto next, auto issued, auto last) {  // `next`: another step follows; `issued`: and one more
+      const int by = decltype(issued)::value ? stride() : 0;
 #pragma unroll
       for (int g = 0; g < kGroups; ++g) {
         const int behind = g - (kGroups - kAhead);  // groups since the barrier
@@ -230,7 +275,7 @@ struct Tile {
           if constexpr (decltype(issued)::value) {
 #pragma unroll
             for (int i = 0; i < kLoads; ++i)
-              if (i * kAhead / kLoads == behind) load(from, last, slot, i);
+              if (i * kAhead / kLoads == behind) load(from, last, slot, i, by);
           }
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -267,7 +312,7 @@ struct Tile {
 // with none 412.  They go past the caches: nobody reads them soon.)
 template <bool F32, class TL, int NC, typename VALUE, typename PLACE>
 __device__ __forceinline__ void store_tile(unsigned lds, int wave, int lane, VALUE value, PLACE place) {
-  constexpr int kBytes = (TL::ST == 2 ? TL::kStage : TL::kLdsBytes) / TL::kWaves;
+  constexpr int kBytes = TL::kStaging / TL::kWaves;
   constexpr int kRow = NC * 16 * (F32 ? 4 : 2);                    // bytes of a row
   constexpr int kFit = kBytes / (16 * kRow);
   constexpr int kPass = kFit < TL::MB ? kFit : TL::MB;             // token blocks at a time

@@ -26,7 +26,7 @@ struct ProjectArgs {
   const int32_t* request_adapters;
   void* out;               // [T, N]
   void* inner;             // v: [T, 3, R] bf16 or [T, R] fp32;  thin: [slices, T, R] fp32, not scaled
-  float* shared;           // thin: [slices, T, N]
+  float* shared;           // thin: [slices, T, N];  more than one slice of tiles: v, [slices, T, R], not scaled
   int32_t* adapter;        // [T] the row's adapter, or -1
   int T, N, M, R, requests;
   int K;                   // bytes of a row of x, w and a_down
@@ -47,10 +47,11 @@ __device__ __forceinline__ int requests_begun(const ProjectArgs& a, int t, int l
   return lo + __popcll(__ballot(lane < len && a.request_offsets[lo + min(lane, max(len - 1, 0))] <= t));
 }
 
-// The adapter of row t0 + lane % 16, or -1.  A row belongs to the last request that begins at or
+// The adapter of row t0 + lane % ROWS, or -1.  A row belongs to the last request that begins at or
 // before it, if that one has not ended.
+template <int ROWS>
 __device__ __forceinline__ int adapter_of_row(const ProjectArgs& a, int t0, int lane) {
-  const int t = t0 + (lane & 15);
+  const int own = lane & (ROWS - 1), t = t0 + own;
   // 64 requests at a time, from the one that row t0 may belong to
   int m = -1;
   for (int at = a.requests <= 64 ? 0 : max(requests_begun(a, t0, lane) - 1, 0); at < a.requests; at += 64) {
@@ -59,13 +60,13 @@ __device__ __forceinline__ int adapter_of_row(const ProjectArgs& a, int t0, int 
     const int begin = a.request_offsets[q], end = a.request_offsets[q + 1], adapter = a.request_adapters[q];
     int n = 0;  // of these, how many begin at or before this lane's row
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
+    for (int i = 0; i < ROWS; ++i) {
       const int c = __popcll(__ballot(is && begin <= t0 + i));
-      if ((lane & 15) == i) n = c;
+      if (own == i) n = c;
     }
     const int last = max(n - 1, 0), its_end = __shfl(end, last), its_adapter = __shfl(adapter, last);
     if (n > 0) m = t < its_end ? its_adapter : -1;
-    if (__ballot(is && begin <= t0 + 15) != ~0ull) break;
+    if (__ballot(is && begin <= t0 + ROWS - 1) != ~0ull) break;
   }
   return t < a.T && (unsigned)m < (unsigned)a.M ? m : -1;
 }
@@ -92,7 +93,7 @@ template <bool F32, int B>
 __device__ __forceinline__ void thin_product(const ThinTokens& head, const unsigned char* tokens,
                                              const unsigned char* const (&rows)[B], int bytes, int begin, int end, int lane,
                                              mma_f32x4 (&acc)[B]) {
-  constexpr int kBatch = B <= 2 ? kThinBatch : 2;
+  constexpr int kBatch = B <= 4 ? kThinBatch : 2;
   for (int k = begin; k < end; k += kBatch) {
     mma_u32x4 t[kBatch], r[kBatch][B];
 #pragma unroll
@@ -108,17 +109,17 @@ __device__ __forceinline__ void thin_product(const ThinTokens& head, const unsig
   }
 }
 
-// The four wavefronts' sums of B blocks, added in their order; value i of thread j is row
-// 4 (lane / 16) + i, token lane % 16 of block wave + 4 n.
-template <int B, typename USE>
+// The WAVES wavefronts' sums of B blocks, added in their order; value i of a lane is row
+// 4 (lane / 16) + i, token lane % 16.
+template <int B, int WAVES, typename USE>
 __device__ __forceinline__ void join_wavefronts(mma_f32x4 (&acc)[B], float* part, int wave, int lane, USE use) {
 #pragma unroll
-  for (int b = 0; b < B; ++b) *reinterpret_cast<mma_f32x4*>(part + ((b * 4 + wave) * 64 + lane) * 4) = acc[b];
+  for (int b = 0; b < B; ++b) *reinterpret_cast<mma_f32x4*>(part + ((b * WAVES + wave) * 64 + lane) * 4) = acc[b];
   __syncthreads();
-  for (int b = wave; b < B; b += 4) {
-    mma_f32x4 sum = *reinterpret_cast<const mma_f32x4*>(part + (b * 4 * 64 + lane) * 4);
+  for (int b = wave; b < B; b += WAVES) {
+    mma_f32x4 sum = *reinterpret_cast<const mma_f32x4*>(part + (b * WAVES * 64 + lane) * 4);
 #pragma unroll
-    for (int w = 1; w < 4; ++w) sum += *reinterpret_cast<const mma_f32x4*>(part + ((b * 4 + w) * 64 + lane) * 4);
+    for (int w = 1; w < WAVES; ++w) sum += *reinterpret_cast<const mma_f32x4*>(part + ((b * WAVES + w) * 64 + lane) * 4);
     use(b, sum);
   }
   __syncthreads();
@@ -133,15 +134,31 @@ __device__ __forceinline__ void split3(float x, unsigned (&piece)[3]) {
   }
 }
 
+// v[t, r .. r + 3] as the second product reads it
+template <bool F32>
+__device__ __forceinline__ void put_inner(const ProjectArgs& a, int t, int r, mma_f32x4 v) {
+  if constexpr (F32) {
+    store4<true>(a.inner, (size_t)t * a.R + r, v);
+  } else {
+    unsigned p[4][3];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) split3(v[i], p[i]);
+#pragma unroll
+    for (int j = 0; j < 3; ++j)
+      *reinterpret_cast<mma_u32x2*>(static_cast<unsigned short*>(a.inner) + ((size_t)t * 3 + j) * a.R + r) =
+          mma_u32x2{p[0][j] | p[1][j] << 16, p[2][j] | p[3][j] << 16};
+  }
+}
+
 // Workgroup (x, y, z): 16 rows, every lanes-th of their distinct adapters from y on, slice z of
-// the contraction axis, cut over the four wavefronts.  THIN: sums of slices, and behind the
+// the contraction axis, cut over the wavefronts.  THIN: sums of slices, and behind the
 // first `lanes` y the shared projection, 16 columns each.
-template <bool F32, int B, bool THIN>
-__global__ __launch_bounds__(256) void adapter_inner_kernel(ProjectArgs a) {
-  __shared__ __align__(16) float part[B * 4 * 256];
+template <bool F32, int B, bool THIN, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void adapter_inner_kernel(ProjectArgs a) {
+  __shared__ __align__(16) float part[B * WAVES * 256];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int t0 = blockIdx.x * 16, t = t0 + (lane & 15);
-  const int steps = (a.K + 63) >> 6, parts = 4 * (THIN ? a.slices : 1), own = (THIN ? 4 * (int)blockIdx.z : 0) + wave;
+  const int steps = (a.K + 63) >> 6, parts = WAVES * (THIN ? a.slices : 1), own = (THIN ? WAVES * (int)blockIdx.z : 0) + wave;
   const int begin = (int)((long long)steps * own / parts), end = (int)((long long)steps * (own + 1) / parts);
   const unsigned char* const tokens = a.x + (size_t)min(t, a.T - 1) * a.K;
   const ThinTokens head(tokens, a.K, begin, end, lane);
@@ -150,7 +167,7 @@ __global__ __launch_bounds__(256) void adapter_inner_kernel(ProjectArgs a) {
     const unsigned char* rows[1] = {a.w + (size_t)min(n0 + (lane & 15), a.N - 1) * a.K};
     mma_f32x4 acc[1] = {mma_f32x4{0.0f, 0.0f, 0.0f, 0.0f}};
     thin_product<F32, 1>(head, tokens, rows, a.K, begin, end, lane, acc);
-    join_wavefronts<1>(acc, part, wave, lane, [&](int, mma_f32x4 sum) {
+    join_wavefronts<1, WAVES>(acc, part, wave, lane, [&](int, mma_f32x4 sum) {
       if (t >= a.T) return;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -160,7 +177,7 @@ __global__ __launch_bounds__(256) void adapter_inner_kernel(ProjectArgs a) {
     });
     return;
   }
-  const int m = adapter_of_row(a, t0, lane);
+  const int m = adapter_of_row<16>(a, t0, lane);
   if (blockIdx.y == 0 && blockIdx.z == 0 && threadIdx.x < 16 && t < a.T) a.adapter[t] = m;
   unsigned todo = (unsigned)__ballot(m >= 0) & 0xffffu;
   for (int nth = 0; todo != 0; ++nth) {
@@ -176,20 +193,13 @@ __global__ __launch_bounds__(256) void adapter_inner_kernel(ProjectArgs a) {
     for (int b = 0; b < B; ++b) acc[b] = mma_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     thin_product<F32, B>(head, tokens, rows, a.K, begin, end, lane, acc);
     const float scale = THIN || a.scales == nullptr ? 1.0f : a.scales[ad];
-    join_wavefronts<B>(acc, part, wave, lane, [&](int b, mma_f32x4 sum) {
+    join_wavefronts<B, WAVES>(acc, part, wave, lane, [&](int b, mma_f32x4 sum) {
       const int r = b * 16 + 4 * (lane >> 4);
       if (!mine || r >= a.R) return;  // (R is a multiple of 4)
-      if constexpr (THIN || F32) {
-        store4<true>(a.inner, ((THIN ? (size_t)blockIdx.z * a.T : 0) + t) * a.R + r, sum * scale);
-      } else {
-        unsigned p[4][3];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) split3(sum[i] * scale, p[i]);
-#pragma unroll
-        for (int j = 0; j < 3; ++j)
-          *reinterpret_cast<mma_u32x2*>(static_cast<unsigned short*>(a.inner) + ((size_t)t * 3 + j) * a.R + r) =
-              mma_u32x2{p[0][j] | p[1][j] << 16, p[2][j] | p[3][j] << 16};
-      }
+      if constexpr (THIN)
+        store4<true>(a.inner, ((size_t)blockIdx.z * a.T + t) * a.R + r, sum);
+      else
+        put_inner<F32>(a, t, r, sum * scale);
     });
   }
 }
@@ -243,6 +253,103 @@ __global__ __launch_bounds__(256) void adapter_join_kernel(ProjectArgs a) {
   else static_cast<unsigned short*>(a.out)[at] = (unsigned short)bf16_bits(y);
 }
 
+// Many rows: tiles of 64 rows against 128 rows of inner matrices at a time, the first adapters that
+// the 64 rows have, then the next, through LDS (blockIdx.z: every lanes-th of those passes).  blockIdx.y: slice of the contraction axis
+// where there are not tiles enough for all compute units; then sums of slices, joined below.
+// (4096 rows, H = 4096, rank 64: 16 rows per workgroup, as thin calls do, read the matrices four times
+// as often and not by whole lines; 41 us, 26 this way.)
+template <bool F32, int RB>
+__global__ __launch_bounds__(512) void adapter_tiles_kernel(ProjectArgs a) {
+  using TL = Tile<F32, 64, 128, 4, 2, 6>;
+  constexpr int kRoom = 8 / RB;
+  extern __shared__ __align__(1024) unsigned char ring[];
+  int* const ids = reinterpret_cast<int*>(ring + TL::kLdsBytes);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // (slices of whole steps)
+  const int steps = (a.K + kStepBytes - 1) / kStepBytes, slice = blockIdx.y;
+  const int begin = (int)((long long)steps * slice / a.slices) * kStepBytes;
+  const int end = min((int)((long long)steps * (slice + 1) / a.slices) * kStepBytes, a.K);
+  TL tile(end - begin, (unsigned)(size_t)(lds_bytes)ring, wave, lane);
+  const int tok = lane & 15, quad = lane >> 4, wm = wave % 4, wn = wave / 4;
+  const int t0 = blockIdx.x * 64;
+  if (wn == 0) {
+    const int m = adapter_of_row<16>(a, t0 + wm * 16, lane), t = t0 + wm * 16 + lane;
+    if (lane < 16) {
+      ids[wm * 16 + lane] = m;
+      if (t < a.T && slice == 0 && blockIdx.z == 0) a.adapter[t] = m;
+    }
+  }
+  lds_barrier();
+  const int id = ids[lane], m = ids[wm * 16 + tok], t = t0 + wm * 16 + tok;
+  unsigned long long todo = __ballot(id >= 0);
+  const unsigned char* from[TL::kLoads];
+  for (int pass = 0; todo != 0; ++pass) {
+    int held[kRoom];
+#pragma unroll
+    for (int q = 0; q < kRoom; ++q) {
+      held[q] = -1;
+      if (todo != 0) {
+        held[q] = __builtin_amdgcn_readlane(id, __builtin_ctzll(todo));
+        todo &= ~__ballot(id == held[q]);
+      }
+    }
+    if (pass % a.lanes != (int)blockIdx.z) continue;
+    tile.turn_to(blockIdx.x);
+    const int piece = TL::piece(wave, lane) * 16 + tile.turn * kStepBytes + begin;
+#pragma unroll
+    for (int i = 0; i < TL::kLoads; ++i) {
+      const int r = TL::row(wave, lane, i);
+      if (r < 64) {
+        from[i] = a.x + (size_t)min(t0 + r, a.T - 1) * a.K + piece;
+      } else {
+        const int x = r - 64, which = x / (16 * RB);  // (the same for all lanes of a load instruction)
+        int ad = -1;
+#pragma unroll
+        for (int q = 0; q < kRoom; ++q) ad = which == q ? held[q] : ad;
+        if (ad < 0) ad = held[0];
+        from[i] = a.a_down + ((size_t)ad * a.R + min(x % (16 * RB), a.R - 1)) * a.K + piece;
+      }
+    }
+    mma_f32x4 acc[4][1];
+#pragma unroll
+    for (int n = 0; n < 4; ++n) acc[n][0] = mma_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    tile.start(from);
+    tile.run(from, 1, acc);
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      const int block = wn * 4 + n, r = block % RB * 16 + 4 * quad;
+      int ad = -1;
+#pragma unroll
+      for (int q = 0; q < kRoom; ++q) ad = block / RB == q ? held[q] : ad;
+      if (ad < 0 || m != ad || r >= a.R) continue;
+      if (a.slices > 1) {
+        store4<true>(a.shared, ((size_t)slice * a.T + t) * a.R + r, acc[n][0]);
+      } else {
+        put_inner<F32>(a, t, r, acc[n][0] * (a.scales != nullptr ? a.scales[ad] : 1.0f));
+      }
+    }
+  }
+}
+
+// The slices' sums of the rows that have an adapter.
+template <bool F32>
+__global__ __launch_bounds__(256) void adapter_slices_kernel(ProjectArgs a) {
+  const int quads = a.R >> 2;
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x, t = i / quads;
+  if (t >= a.T) return;
+  const int m = a.adapter[t], r = (int)(i - t * quads) * 4;
+  if (m < 0) return;
+  mma_f32x4 part[kThinSlices];
+#pragma unroll
+  for (int s = 0; s < kThinSlices; ++s)
+    part[s] = s < a.slices ? *reinterpret_cast<const mma_f32x4*>(a.shared + ((size_t)s * a.T + t) * a.R + r)
+                           : mma_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  mma_f32x4 sum = part[0];
+#pragma unroll
+  for (int s = 1; s < kThinSlices; ++s) sum += part[s];
+  put_inner<F32>(a, (int)t, r, sum * (a.scales != nullptr ? a.scales[m] : 1.0f));
+}
+
 // U v added to a wavefront's accumulators: per block of 16 tokens and distinct adapter in it, 32
 // values of v at a time (fp32: 16), the rows of other adapters as zeros.
 template <bool F32, class TL>
@@ -250,6 +357,7 @@ __device__ __forceinline__ void add_adapters(const ProjectArgs& a, int t0, int n
                                              mma_f32x4 (&acc)[TL::NB][TL::MB]) {
   constexpr int NB = TL::NB, MB = TL::MB, kPieces = F32 ? 1 : 3;
   constexpr int kSize = F32 ? 4 : 2, kOwn = 16 / kSize;  // values of v that a lane holds at a time
+  constexpr int kAhead = MB < 2 ? MB : 2;
   int ids[MB];
   bool any = false;
 #pragma unroll
@@ -263,17 +371,22 @@ __device__ __forceinline__ void add_adapters(const ProjectArgs& a, int t0, int n
     const int r = r0 + (lane >> 4) * kOwn;
     const bool in = r < a.R;
     int held = -1;  // the adapter whose rows are in u
-    mma_u32x4 u[NB];
+    mma_u32x4 u[NB], ahead[kAhead][kPieces];
 #pragma unroll
     for (int m = 0; m < MB; ++m) {
+      if (m % kAhead == 0) {  // v of the next blocks, all under way at once
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+          const int t = min(t0 + TL::block_row(wave, min(m + k, MB - 1)) + (lane & 15), a.T - 1);
+#pragma unroll
+          for (int j = 0; j < kPieces; ++j)
+            ahead[k][j] = *reinterpret_cast<const mma_u32x4*>(static_cast<const unsigned char*>(a.inner) +
+                                                              (((size_t)t * kPieces + j) * a.R + (in ? r : 0)) * kSize);
+        }
+      }
       unsigned todo = (unsigned)__ballot(ids[m] >= 0) & 0xffffu;
       if (todo == 0) continue;
-      const int t = min(t0 + TL::block_row(wave, m) + (lane & 15), a.T - 1);
-      mma_u32x4 v[kPieces];
-#pragma unroll
-      for (int j = 0; j < kPieces; ++j)
-        v[j] = *reinterpret_cast<const mma_u32x4*>(static_cast<const unsigned char*>(a.inner) +
-                                                   (((size_t)t * kPieces + j) * a.R + (in ? r : 0)) * kSize);
+      mma_u32x4 (&v)[kPieces] = ahead[m % kAhead];
       while (todo != 0) {
         const int ad = __builtin_amdgcn_readlane(ids[m], __builtin_ctz(todo));
         const bool mine = ids[m] == ad;
@@ -344,14 +457,15 @@ __global__ __launch_bounds__(TL::kThreads) void project_kernel(ProjectArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int nt = (a.N + BN - 1) / BN, mt = (a.T + BM - 1) / BM, total = mt * nt;
   const int wn = wave / TL::WM;
-  const TL tile(a.K, lds, wave, lane);
+  TL tile(a.K, lds, wave, lane);
   for (int v = blockIdx.x; v < total; v += gridDim.x) {
     const int id = xcd_run(v, total);
     constexpr int kGroup = 8;
     const int g = id / (kGroup * nt), gm = min(kGroup, mt - g * kGroup), in = id - g * kGroup * nt;
     const int t0 = (g * kGroup + in % gm) * BM, n0 = in / gm * BN + wn * (BN / TL::WN);
     const unsigned char* from[TL::kLoads];
-    const int piece = TL::piece(wave, lane) * 16;
+    tile.turn_to(v);
+    const int piece = TL::piece(wave, lane) * 16 + tile.turn * kStepBytes;
 #pragma unroll
     for (int i = 0; i < TL::kLoads; ++i) {
       const int r = TL::row(wave, lane, i);
@@ -384,26 +498,28 @@ __global__ __launch_bounds__(TL::kThreads) void project_kernel(ProjectArgs a) {
 // reads x a second time; bound by reading x, 13 us at the rate of a large copy.)
 constexpr int kNarrowColumns = 64, kNarrowRank = 64;
 template <bool F32, bool OUT32, int RB>  // RB: blocks of 16 that hold an adapter's rows
-__global__ __launch_bounds__(256) void project_narrow_kernel(ProjectArgs a) {
-  using TL = Tile<F32, 64, 128, 4, 1, 6>;
+__global__ __launch_bounds__(512) void project_narrow_kernel(ProjectArgs a) {
+  using TL = Tile<F32, 64, 128, 4, 2, 6>;
   constexpr int kRoom = 4 / RB;  // adapters beside W, twice that without
   extern __shared__ __align__(1024) unsigned char ring[];
   int* const ids = reinterpret_cast<int*>(ring + TL::kLdsBytes);
+  mma_f32x4* const found = reinterpret_cast<mma_f32x4*>(ring);  // v between the passes' products: [4 x 16 rows][8 blocks][lane]
   const unsigned lds = (unsigned)(size_t)(lds_bytes)ring;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const TL tile(a.K, lds, wave, lane);
-  const int tok = lane & 15, quad = lane >> 4;
+  TL tile(a.K, lds, wave, lane);
+  const int tok = lane & 15, quad = lane >> 4, wm = wave % 4, wn = wave / 4;
   const int tiles = (a.T + 63) >> 6;
   for (int v = blockIdx.x; v < tiles; v += gridDim.x) {
     const int t0 = xcd_run(v, tiles) * 64, rows = min(a.T - t0, 64);
-    const int m = adapter_of_row(a, t0 + wave * 16, lane);
-    if (lane < 16) ids[wave * 16 + lane] = m;
+    if (wn == 0) {
+      const int m = adapter_of_row<16>(a, t0 + wm * 16, lane);
+      if (lane < 16) ids[wm * 16 + lane] = m;
+    }
     lds_barrier();
-    const int id = ids[lane];  // of row t0 + lane
+    const int id = ids[lane], m = ids[wm * 16 + tok];  // of row t0 + lane; of this lane's token
     unsigned long long todo = __ballot(id >= 0);
     const unsigned char* from[TL::kLoads];
-    const int piece = TL::piece(wave, lane) * 16;
-    mma_f32x4 y[4][1];  // the tile's results
+    mma_f32x4 y[4][1];  // the tile's results (wavefronts 0 .. 3)
     for (bool first = true; first || todo != 0; first = false) {
       // the adapters of this pass, in order; rows of inner matrices that are not needed repeat others
       int held[2 * kRoom];
@@ -415,6 +531,8 @@ __global__ __launch_bounds__(256) void project_narrow_kernel(ProjectArgs a) {
           todo &= ~__ballot(id == held[q]);
         }
       }
+      tile.turn_to(v);
+      const int piece = TL::piece(wave, lane) * 16 + tile.turn * kStepBytes;
 #pragma unroll
       for (int i = 0; i < TL::kLoads; ++i) {
         const int r = TL::row(wave, lane, i), w = r - 64;  // (rows 0 .. 63 are tokens)
@@ -431,11 +549,20 @@ __global__ __launch_bounds__(256) void project_narrow_kernel(ProjectArgs a) {
           from[i] = (ad < 0 ? a.w : a.a_down + ((size_t)ad * a.R + min(x % (16 * RB), a.R - 1)) * a.K) + piece;
         }
       }
-      mma_f32x4 acc[8][1];
+      mma_f32x4 acc[4][1];
 #pragma unroll
-      for (int n = 0; n < 8; ++n) acc[n][0] = mma_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      for (int n = 0; n < 4; ++n) acc[n][0] = mma_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
       tile.start(from);
       tile.run(from, 1, acc);
+      // v to the wavefronts that have the columns
+      if (!first || wn == 1)
+#pragma unroll
+        for (int n = 0; n < 4; ++n) found[(wm * 8 + (first ? 0 : wn * 4) + n) * 64 + lane] = acc[n][0];
+      lds_barrier();
+      if (wn == 1) {
+        lds_barrier();
+        continue;
+      }
       if (first)
 #pragma unroll
         for (int n = 0; n < 4; ++n) y[n][0] = acc[n][0];
@@ -452,8 +579,7 @@ __global__ __launch_bounds__(256) void project_narrow_kernel(ProjectArgs a) {
           mma_f32x4 inner[2];  // blocks b and, bf16, b + 1
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const int n = q * RB + min(b + h, RB - 1);
-            inner[h] = first ? acc[(4 + n) & 7][0] : acc[n & 7][0];
+            inner[h] = found[(wm * 8 + q * RB + min(b + h, RB - 1)) * 64 + lane];
 #pragma unroll
             for (int i = 0; i < 4; ++i) inner[h][i] = mine && b + h < RB ? inner[h][i] * scale : 0.0f;
           }
@@ -500,8 +626,9 @@ __global__ __launch_bounds__(256) void project_narrow_kernel(ProjectArgs a) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) y[n][0][i] += mine ? d[n][i] : 0.0f;
       }
+      lds_barrier();
     }
-    store_columns<OUT32, TL, 4>(a, lds, wave, lane, t0, rows, 0, y);
+    if (wn == 0) store_columns<OUT32, TL, 4>(a, lds, wave, lane, t0, rows, 0, y);
     lds_barrier();  // (the ring and the ids are free again)
   }
 }
@@ -512,6 +639,9 @@ constexpr int kThinRows = 512, kThinValues = 1 << 16;
 static bool is_thin(int T, int N) { return T <= kThinRows && (long long)T * N <= kThinValues; }
 
 static size_t whole(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
+// Slices of the contraction axis of the inner values' tiles: workgroups for all compute units
+constexpr int kTileWorkgroups = 256;
+static int tile_slices(int T) { return max(1, min(kThinSlices, kTileWorkgroups / ((T + 63) / 64))); }
 struct ProjectLayout {
   size_t adapter, inner, shared, total;
 };
@@ -522,7 +652,9 @@ static ProjectLayout project_layout(int T, int N, const laser_adapter_params_t* 
   L.adapter = 0;
   L.inner = whole((size_t)T * 4);
   L.shared = L.inner + whole((size_t)T * p->rank * per_value);
-  L.total = L.shared + (thin ? whole((size_t)T * N * 4 * kThinSlices) : 0) + 256;
+  // (tiles: rows times slices, see tile_slices, at most; a size that grows with T)
+  const size_t sliced = T > kThinRows ? min((size_t)T * kThinSlices, (size_t)kTileWorkgroups * 64) : 0;
+  L.total = L.shared + 256 + whole(thin ? (size_t)T * N * 4 * kThinSlices : sliced * p->rank * 4);
   return L;
 }
 
@@ -542,14 +674,16 @@ static int check_project(int32_t T, int32_t H, int32_t N, const laser_adapter_pa
 
 template <bool F32, bool THIN>
 static hipError_t launch_inner(const ProjectArgs& a, dim3 grid, hipStream_t s) {
+  // (thin calls have slices enough)
+  constexpr int kWaves = THIN ? 4 : 8;
   if (a.R <= 16)
-    hipLaunchKernelGGL((adapter_inner_kernel<F32, 1, THIN>), grid, dim3(256), 0, s, a);
+    hipLaunchKernelGGL((adapter_inner_kernel<F32, 1, THIN, kWaves>), grid, dim3(64 * kWaves), 0, s, a);
   else if (a.R <= 32)
-    hipLaunchKernelGGL((adapter_inner_kernel<F32, 2, THIN>), grid, dim3(256), 0, s, a);
+    hipLaunchKernelGGL((adapter_inner_kernel<F32, 2, THIN, kWaves>), grid, dim3(64 * kWaves), 0, s, a);
   else if (a.R <= 64)
-    hipLaunchKernelGGL((adapter_inner_kernel<F32, 4, THIN>), grid, dim3(256), 0, s, a);
+    hipLaunchKernelGGL((adapter_inner_kernel<F32, 4, THIN, kWaves>), grid, dim3(64 * kWaves), 0, s, a);
   else
-    hipLaunchKernelGGL((adapter_inner_kernel<F32, 8, THIN>), grid, dim3(256), 0, s, a);
+    hipLaunchKernelGGL((adapter_inner_kernel<F32, 8, THIN, kWaves>), grid, dim3(64 * kWaves), 0, s, a);
   return hipGetLastError();
 }
 
@@ -565,14 +699,37 @@ static hipError_t launch_tiles(const ProjectArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <bool F32, bool OUT32>
+static hipError_t launch_shared(const ProjectArgs& a, hipStream_t s) {
+  if constexpr (!F32)
+    if ((long long)((a.T + 255) / 256) * ((a.N + 255) / 256) >= compute_units() / 2)
+      return launch_tiles<F32, OUT32, Tile<F32, 256, 256, 2, 4, 2>>(a, s);
+  return launch_tiles<F32, OUT32, Tile<F32, 64, 64, 1, 4, 4>>(a, s);
+}
+
+template <bool F32, int RB>
+static hipError_t launch_inner_tiles(const ProjectArgs& a, hipStream_t s) {
+  static LdsAttr attr;
+  constexpr int kLds = Tile<F32, 64, 128, 4, 2, 6>::kLdsBytes + 64 * 4;
+  const void* fn = reinterpret_cast<const void*>(&adapter_tiles_kernel<F32, RB>);
+  hipError_t err = allow_dynamic_lds(fn, kLds, attr);
+  if (err != hipSuccess) return err;
+  hipLaunchKernelGGL((adapter_tiles_kernel<F32, RB>), dim3((a.T + 63) / 64, a.slices, a.lanes), dim3(512), kLds, s, a);
+  err = hipGetLastError();
+  if (err != hipSuccess || a.slices == 1) return err;
+  const unsigned grid = (unsigned)(((long long)a.T * (a.R / 4) + 255) / 256);
+  hipLaunchKernelGGL((adapter_slices_kernel<F32>), dim3(grid), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
 template <bool F32, bool OUT32, int RB>
 static hipError_t launch_narrow(const ProjectArgs& a, hipStream_t s) {
   static LdsAttr attr;
-  constexpr int kLds = Tile<F32, 64, 128, 4, 1, 6>::kLdsBytes + 64 * 4;
+  constexpr int kLds = Tile<F32, 64, 128, 4, 2, 6>::kLdsBytes + 64 * 4;
   const void* fn = reinterpret_cast<const void*>(&project_narrow_kernel<F32, OUT32, RB>);
   hipError_t err = allow_dynamic_lds(fn, kLds, attr);
   if (err != hipSuccess) return err;
-  hipLaunchKernelGGL((project_narrow_kernel<F32, OUT32, RB>), dim3(min((a.T + 63) / 64, 1 << 20)), dim3(256), kLds, s, a);
+  hipLaunchKernelGGL((project_narrow_kernel<F32, OUT32, RB>), dim3(min((a.T + 63) / 64, 1 << 20)), dim3(512), kLds, s, a);
   return hipGetLastError();
 }
 
@@ -589,18 +746,25 @@ static hipError_t launch_project(ProjectArgs& a, hipStream_t s) {
     hipLaunchKernelGGL((adapter_join_kernel<F32, OUT32>), dim3(a.T, (a.N + threads - 1) / threads), dim3(threads), 0, s, a);
     return hipGetLastError();
   }
-  if (a.N <= kNarrowColumns && a.R <= kNarrowRank)
+  // (a tile of a gate makes its passes one after the other: not where many requests may meet in it)
+  if (a.N <= kNarrowColumns && a.R <= kNarrowRank && (a.requests <= 32 || a.requests <= a.T / 64))
     return a.R <= 16   ? launch_narrow<F32, OUT32, 1>(a, s)
            : a.R <= 32 ? launch_narrow<F32, OUT32, 2>(a, s)
                        : launch_narrow<F32, OUT32, 4>(a, s);
+  if (a.T > kThinRows) {
+    a.slices = min(tile_slices(a.T), (a.K + kStepBytes - 1) / kStepBytes);
+    // (few requests seldom meet in a tile; where many do, its passes are shared)
+    a.lanes = a.requests <= 32 ? 1 : 4;
+    const hipError_t err = a.R <= 16 ? launch_inner_tiles<F32, 1>(a, s) : a.R <= 32 ? launch_inner_tiles<F32, 2>(a, s)
+                           : a.R <= 64 ? launch_inner_tiles<F32, 4>(a, s) : launch_inner_tiles<F32, 8>(a, s);
+    if (err != hipSuccess) return err;
+    return launch_shared<F32, OUT32>(a, s);
+  }
   a.slices = 1;
   a.lanes = a.requests > 0 ? min(min(16, a.requests), max(1, 1024 / rows16)) : 1;
   hipError_t err = launch_inner<F32, false>(a, dim3(rows16, a.lanes, 1), s);
   if (err != hipSuccess) return err;
-  if constexpr (!F32)
-    if ((long long)((a.T + 255) / 256) * ((a.N + 255) / 256) >= compute_units() / 2)
-      return launch_tiles<F32, OUT32, Tile<F32, 256, 256, 2, 4, 2>>(a, s);
-  return launch_tiles<F32, OUT32, Tile<F32, 64, 64, 1, 4, 4>>(a, s);
+  return launch_shared<F32, OUT32>(a, s);
 }
 
 }  // namespace laser

@@ -31,6 +31,9 @@ SHAPES = [
     (513, 136, 24, 24, 700, [1] * 300 + [0, 0] * 100 + [3] * 71),   # hundreds of requests, many of them empty
     (600, 136, 130, 104, 5, [0] * 70 + [5] * 40 + [0] * 5000 + [400]),
     (700, 264, 40, 64, 6, [1] * 70 + [5, 60, 65, 500]),              # many adapters in a tile of a gate
+    (530, 1032, 200, 128, 40, [1] * 64 + [100, 3, 3, 300]),
+    (2100, 328, 72, 16, 50, [1] * 130 + [2] * 20 + [1900]),
+    (900, 8, 96, 8, 3, [300, 300]),                                  # one step, no slices
     (1200, 136, 64, 48, 9, [400, 1, 1, 1, 797]),
     (4200, 200, 2061, 40, 6, [900, 20, 1, 2000, 1279]),              # the widest tiles, odd columns
     (4100, 72, 2560, 128, 3, [1024, 1, 3075]),
@@ -135,7 +138,8 @@ def test_the_workspace_serves_every_smaller_call():
     for N in (1, 64, 130, 5000, 200_000):
         for R, dtype in ((8, BF16), (128, BF16), (64, F32)):
             p = B.make_adapter_params(R, 2, 3, dtype=dtype)
-            sizes = [B.laser_project_workspace_bytes(T, 64, N, p) for T in (0, 1, 12, 13, 512, 513, 1024, 1025, 5000)]
+            sizes = [B.laser_project_workspace_bytes(T, 64, N, p) for T in (0, 1, 12, 13, 512, 513, 1024, 1025, 2048, 2049, 5000,
+                                                                               16384, 16385, 20000)]
             assert sizes == sorted(sizes)
 
 
