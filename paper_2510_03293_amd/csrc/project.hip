@@ -260,7 +260,7 @@ __global__ __launch_bounds__(256) void adapter_join_kernel(ProjectArgs a) {
 // as often and not by whole lines; 41 us, 26 this way.)
 template <bool F32, int RB>
 __global__ __launch_bounds__(512) void adapter_tiles_kernel(ProjectArgs a) {
-  using TL = Tile<F32, 64, 128, 4, 2, 6>;
+  using TL = Tile<F32, 64, 128, 4, 2, 3>;
   constexpr int kRoom = 8 / RB;
   extern __shared__ __align__(1024) unsigned char ring[];
   int* const ids = reinterpret_cast<int*>(ring + TL::kLdsBytes);
@@ -426,7 +426,7 @@ __device__ __forceinline__ void store_columns(const ProjectArgs& a, unsigned lds
                                               mma_f32x4 (&y)[NC][TL::MB]) {
   constexpr int kSize = OUT32 ? 4 : 2;
   if (a.N % (16 / kSize) == 0) {
-    store_tile<OUT32, TL, NC>(
+    store_tile<OUT32 ? kF32 : kBf16, TL, NC>(
         lds, wave, lane, [&](int n, int m) { return y[n][m]; },
         [&](int r, int c) -> void* {
           return r < rows && n0 + c < a.N ? static_cast<char*>(a.out) + ((size_t)(t0 + r) * a.N + n0 + c) * kSize : nullptr;
@@ -710,7 +710,7 @@ static hipError_t launch_shared(const ProjectArgs& a, hipStream_t s) {
 template <bool F32, int RB>
 static hipError_t launch_inner_tiles(const ProjectArgs& a, hipStream_t s) {
   static LdsAttr attr;
-  constexpr int kLds = Tile<F32, 64, 128, 4, 2, 6>::kLdsBytes + 64 * 4;
+  constexpr int kLds = Tile<F32, 64, 128, 4, 2, 3>::kLdsBytes + 64 * 4;
   const void* fn = reinterpret_cast<const void*>(&adapter_tiles_kernel<F32, RB>);
   hipError_t err = allow_dynamic_lds(fn, kLds, attr);
   if (err != hipSuccess) return err;
@@ -753,8 +753,9 @@ static hipError_t launch_project(ProjectArgs& a, hipStream_t s) {
                        : launch_narrow<F32, OUT32, 4>(a, s);
   if (a.T > kThinRows) {
     a.slices = min(tile_slices(a.T), (a.K + kStepBytes - 1) / kStepBytes);
-    // (few requests seldom meet in a tile; where many do, its passes are shared)
-    a.lanes = a.requests <= 32 ? 1 : 4;
+    // (a tile's passes side by side; workgroups without one end at once.  Rank 128, 16384 rows of 40
+    // requests: 143 us with one, 126 with four)
+    a.lanes = max(1, min(a.requests, 4));
     const hipError_t err = a.R <= 16 ? launch_inner_tiles<F32, 1>(a, s) : a.R <= 32 ? launch_inner_tiles<F32, 2>(a, s)
                            : a.R <= 64 ? launch_inner_tiles<F32, 4>(a, s) : launch_inner_tiles<F32, 8>(a, s);
     if (err != hipSuccess) return err;

@@ -97,6 +97,13 @@ def down_reference(act, w_down, perm, offs, ids, weights, base, k, first, T, dty
         np.add.at(out, slots // k, z * wt[:, None])
         np.add.at(tol, slots // k, (bz + U * np.abs(z)) * np.abs(wt)[:, None])
         np.add.at(size, slots // k, np.abs(z * wt[:, None]))
+    # bf16: a summand may be held in fp16 after a power of two has brought the largest of its row's 64
+    # columns to 2^14 or more.  fp16 values have 11 significant bits, so rounding is off by half of
+    # 2^-10 of the value, 2^-11; below 2^-14 it is off by half of its step of 2^-24, which is 2^-25 / 2^14 =
+    # 2^-39 of the largest.
+    if dtype == B.DTYPE_BF16:
+        own = size if base is None else size - np.abs(f64(base))
+        tol += 2.0 ** -11 * own + 2.0 ** -39 * own.max(axis=1, keepdims=True) * k
     # k additions (and the base's) of partial sums no larger than the sum of magnitudes
     return out, (tol + (k + 1) * U * size) * 1.01 + HALF_STEP[dtype] * np.abs(out) * 1.01 + 1e-37
 
