@@ -1,4 +1,6 @@
 // The experts of a layer over the routing tables: laser_experts_up and laser_experts_down.
+#include <algorithm>
+
 #include "../../include/laser.h"
 #include "grouped.h"
 
@@ -9,7 +11,7 @@ namespace laser {
 // columns; a summand is then off by 2^-11 of itself (and 2^-39 of the largest of its kShared), while
 // out is rounded by 2^-8 of the sum, so that what a call is off by does not change in two
 // digits.  The sum itself is taken in fp32.  Written and read once each, these values are the largest part of
-// a large call's traffic: 16384 tokens, 6 of 64 experts, H = 2048, F = 1408: ZTIME32 us with fp32, ZTIME16 so.
+// a large call's traffic: 16384 tokens, 6 of 64 experts, H = 2048, F = 1408: 811 us with fp32, 730 so.
 // (bf16 would do without factors but be off by 2^-8, which is seen in out.)
 constexpr int kShared = 64;
 __host__ __device__ inline int shared_blocks(int H) { return (H + kShared - 1) / kShared; }
@@ -30,9 +32,10 @@ struct ExpertArgs {
   int H;       // experts_down: columns of out
 };
 
-// Which expert tile `mt` of BM rows belongs to: per lane one expert, tiles counted in order.
+// The call's experts, one per lane: where their positions begin, how many there are, and, for tiles of
+// BM rows, how many tiles the experts before have.
 struct ExpertTiles {
-  int lo, cnt, before, total;  // this lane's expert: first position, positions, tiles of earlier experts
+  int lo, cnt, before, total;
   __device__ void init(const ExpertArgs& a, int lane) {
     if (a.offsets == nullptr) {
       lo = 0;
@@ -41,6 +44,17 @@ struct ExpertTiles {
       // (offsets are the caller's: whatever they hold, positions stay inside the tables)
       lo = lane < a.E ? min(max(a.offsets[lane], 0), a.slots) : 0;
       cnt = lane < a.E ? max(min(a.offsets[lane + 1], a.slots) - lo, 0) : 0;
+      if (a.slots > 1 << 24) {
+        // (... and sums of what they may hold do not pass 32 bits: no position twice)
+        int end = lo + cnt;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) end = max(end, __shfl_up(end, d));
+        const int before_me = __shfl_up(end, 1);
+        if (lane > 0) {
+          cnt = max(lo + cnt - max(lo, before_me), 0);
+          lo = max(lo, before_me);
+        }
+      }
     }
   }
   __device__ void count(int lane, int BM) {
@@ -54,12 +68,18 @@ struct ExpertTiles {
     before = sum - tiles;
     total = __builtin_amdgcn_readlane(sum, 63);
   }
-  // expert, first position and rows of tile mt < total
-  __device__ void find(int mt, int BM, int& e, int& p0, int& rows) const {
-    e = 63 - __builtin_clzll(__ballot(before <= mt && cnt > 0));
-    const int in = (mt - __builtin_amdgcn_readlane(before, e)) * BM;
-    p0 = __builtin_amdgcn_readlane(lo, e) + in;
-    rows = min(__builtin_amdgcn_readlane(cnt, e) - in, BM);
+  // Tile `id` < total * nt of an order that goes expert by expert, so that the tiles which run side
+  // by side share its rows: up to kGroup tiles of rows walk its nt tiles of columns together.
+  __device__ void find(int id, int nt, int BM, int& e, int& p0, int& rows, int& column) const {
+    constexpr int kGroup = 8;
+    e = 63 - __builtin_clzll(__ballot(cnt > 0 && before <= id / nt));
+    const int n = __builtin_amdgcn_readlane(cnt, e), mts = (n + BM - 1) / BM;
+    const int in_e = id - __builtin_amdgcn_readlane(before, e) * nt;
+    const int g = in_e / (kGroup * nt), gm = min(kGroup, mts - g * kGroup), in = in_e - g * kGroup * nt;
+    column = in / gm;
+    const int row = (g * kGroup + in - column * gm) * BM;
+    p0 = __builtin_amdgcn_readlane(lo, e) + row;
+    rows = min(n - row, BM);
   }
 };
 
@@ -92,11 +112,9 @@ __device__ __forceinline__ void experts_tiles(const ExpertArgs& a, unsigned char
 
   int e, p0, rows, c0;
   auto find = [&](int v) {
-    const int id = xcd_run(v, total);
-    constexpr int kGroup = 8;  // tiles of rows that walk the columns together
-    const int g = id / (kGroup * nt), gm = min(kGroup, tiles.total - g * kGroup), in = id - g * kGroup * nt;
-    c0 = in / gm * kCols;
-    tiles.find(g * kGroup + in % gm, BM, e, p0, rows);
+    int column;
+    tiles.find(xcd_run(v, total), nt, BM, e, p0, rows, column);
+    c0 = column * kCols;
   };
   // this thread's row of the tile: its slot (rows past the end repeat the last one)
   auto slot_of = [&]() {
@@ -246,7 +264,7 @@ __global__ __launch_bounds__(TL::kThreads) void experts_kernel(ExpertArgs a, int
   tiles.init(a, lane);
   if (rows != 0) {
     tiles.count(lane, 1);
-    if ((tiles.total >= (long long)rows * __popcll(__ballot(tiles.cnt > 0))) != MANY) return;
+    if ((tiles.total >= (long long)rows * a.E) != MANY) return;
   }
   experts_tiles<F32, UP, TL>(a, ring, tiles, lane, wave);
 }
@@ -344,16 +362,17 @@ __global__ __launch_bounds__(256) void experts_up_few_kernel(ExpertArgs a) {
   }
 }
 
-// kFewRows rows of out (columns, for the caller) per workgroup.  Its wavefronts take the slots
+// ROWS rows of the matrices (columns of out) per workgroup, eight unless there are not enough for all
+// compute units.  Its wavefronts take the slots
 // in turn, and where there are fewer slots than wavefronts, parts of the rows as well; what they
 // find waits in LDS for its place in the sums, which run in slot order.
-constexpr int kFewRows = 8, kFewWaves = 8;
-template <bool F32>
+constexpr int kFewWaves = 8;
+template <bool F32, int ROWS>
 __global__ __launch_bounds__(64 * kFewWaves) void experts_down_few_kernel(ExpertArgs a, const int32_t* ids, int first,
                                                                           const void* base, void* out, int T) {
-  __shared__ float found[kFewSlots * kFewRows];
+  __shared__ float found[kFewSlots * ROWS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int h0 = blockIdx.x * kFewRows;
+  const int h0 = blockIdx.x * ROWS;
   ExpertTiles tiles;
   tiles.init(a, lane);
   // the slot at this lane's position (positions and slots: one per lane)
@@ -366,22 +385,22 @@ __global__ __launch_bounds__(64 * kFewWaves) void experts_down_few_kernel(Expert
     const unsigned long long where = __ballot(at == slot);
     const int p = where == 0 ? -1 : __builtin_ctzll(where);
     const int e = p < 0 ? -1 : expert_of(tiles, p);
-    float sum[kFewRows] = {};
+    float sum[ROWS] = {};
     if (e >= 0 && mine(slot)) {
-      const unsigned char* row[kFewRows];
+      const unsigned char* row[ROWS];
 #pragma unroll
-      for (int r = 0; r < kFewRows; ++r) row[r] = a.w + ((size_t)e * a.H + min(h0 + r, a.H - 1)) * a.K;
-      row_products<F32, kFewRows, 3>(row, a.x + (size_t)p * a.K, a.K, chunks * part / parts, chunks * (part + 1) / parts,
+      for (int r = 0; r < ROWS; ++r) row[r] = a.w + ((size_t)e * a.H + min(h0 + r, a.H - 1)) * a.K;
+      row_products<F32, ROWS, 3>(row, a.x + (size_t)p * a.K, a.K, chunks * part / parts, chunks * (part + 1) / parts,
                                      lane, sum);
     }
 #pragma unroll
-    for (int r = 0; r < kFewRows; ++r) {
+    for (int r = 0; r < ROWS; ++r) {
       const float s = lanes_sum(sum[r]);
-      if (lane == 0) found[u * kFewRows + r] = s;
+      if (lane == 0) found[u * ROWS + r] = s;
     }
   }
   __syncthreads();
-  const int r = threadIdx.x % kFewRows, t = threadIdx.x / kFewRows, h = h0 + r;
+  const int r = threadIdx.x % ROWS, t = threadIdx.x / ROWS, h = h0 + r;
   if (t >= T || h >= a.H) return;
   float y = 0.0f;
   if (base != nullptr)
@@ -390,7 +409,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void experts_down_few_kernel(Expert
   for (int slot = t * a.k; slot < (t + 1) * a.k; ++slot) {
     if (!mine(slot)) continue;
     float z = 0.0f;
-    for (int part = 0; part < parts; ++part) z += found[(slot * parts + part) * kFewRows + r];
+    for (int part = 0; part < parts; ++part) z += found[(slot * parts + part) * ROWS + r];
     y += z * (a.weights != nullptr ? a.weights[slot] : 1.0f);
   }
   if constexpr (F32) static_cast<float*>(out)[(size_t)t * a.H + h] = y;
@@ -457,7 +476,7 @@ constexpr int lds_of() { return TL::kLdsBytes + TL::BM * 12; }  // the ring, and
 template <class TL, bool UP>
 static long long grid_of(const ExpertArgs& a) {
   // (every expert with rows has at most one tile that is not full, and every tile a row)
-  const long long mt = min((long long)a.slots, (long long)a.slots / TL::BM + min(a.E, a.slots));
+  const long long mt = std::min<long long>(a.slots, a.slots / TL::BM + std::min(a.E, a.slots));
   const int cols = UP ? TL::BN / 2 : TL::BN;
   return mt * (((UP ? a.F : a.H) + cols - 1) / cols);
 }
@@ -468,7 +487,7 @@ static hipError_t launch_experts(const ExpertArgs& a, int rows, long long most, 
   const void* fn = reinterpret_cast<const void*>(&experts_kernel<F32, UP, TL, MANY>);
   hipError_t err = allow_dynamic_lds(fn, lds_of<TL>(), attr);
   if (err != hipSuccess) return err;
-  const unsigned grid = (unsigned)min(grid_of<TL, UP>(a), most);
+  const unsigned grid = (unsigned)std::min(grid_of<TL, UP>(a), most);
   hipLaunchKernelGGL((experts_kernel<F32, UP, TL, MANY>), dim3(grid), dim3(TL::kThreads), lds_of<TL>(), s, a, rows);
   return hipGetLastError();
 }
@@ -483,7 +502,10 @@ static hipError_t launch_experts(const ExpertArgs& a, int rows, long long most, 
 // are tiles for all compute units; before that, small tiles are more of them (333 tokens, 33
 // experts, 516 x 212: 30 us with tiles of 64 x 128, 20 with 32 x 64; 4000 tokens, 8 experts,
 // 1024 x 1024: 333 and 391).
-constexpr int kSomeRows = 96, kManyRows = 160;
+// With few steps what comes before and behind them counts, of which two workgroups of a compute unit
+// hide each other's (8000 tokens, 2000 rows per expert, 128 x 128 and 256 x 256: down of F = 320 70, 76,
+// F = 1024 109, 116; up of H = 136 62, 80, H = 640 103, 102, H = 1024 145, 141).
+constexpr int kSomeRows = 96, kManyRows = 160, kWideSteps = 18;
 template <bool F32, bool UP>
 static hipError_t launch_products(const ExpertArgs& a, hipStream_t s) {
   using LOW = Tile<F32, 64, 128, 2, 2, 3>;
@@ -491,11 +513,12 @@ static hipError_t launch_products(const ExpertArgs& a, hipStream_t s) {
     if (grid_of<LOW, UP>(a) < compute_units())
       return launch_experts<F32, UP, Tile<F32, 32, 64, 2, 2, 6>, false>(a, 0, kGridMost, s);
   } else if (a.slots >= (long long)kSomeRows * a.E) {
-    if (a.slots >= kManyRows) {
+    const bool wide = a.slots >= kManyRows && a.K >= kWideSteps * kStepBytes;
+    if (wide) {
       const hipError_t err = launch_experts<F32, UP, Tile<F32, 256, 256, 2, 4, 2>, true>(a, kManyRows, compute_units(), s);
       if (err != hipSuccess) return err;
     }
-    return launch_experts<F32, UP, Tile<F32, 128, 128, 2, 2, 2>, false>(a, kManyRows, 4 * compute_units(), s);
+    return launch_experts<F32, UP, Tile<F32, 128, 128, 2, 2, 2>, false>(a, wide ? kManyRows : 0, 4 * compute_units(), s);
   }
   return launch_experts<F32, UP, LOW, false>(a, 0, kGridMost, s);
 }
@@ -607,19 +630,21 @@ extern "C" int laser_experts_down(const void* act, const void* w_down, int32_t T
   clear_stale_error();
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   if (are_few(T, a.slots, F)) {
-    const dim3 grid((H + kFewRows - 1) / kFewRows);
-    if (f32)
-      hipLaunchKernelGGL((experts_down_few_kernel<true>), grid, dim3(64 * kFewWaves), 0, s, a, expert_ids,
-                         params->first_expert, base, out, T);
-    else
-      hipLaunchKernelGGL((experts_down_few_kernel<false>), grid, dim3(64 * kFewWaves), 0, s, a, expert_ids,
-                         params->first_expert, base, out, T);
+    const int rows = H >= 8 * compute_units() ? 8 : H >= 4 * compute_units() ? 4 : 2;
+    const dim3 grid((H + rows - 1) / rows), block(64 * kFewWaves);
+    auto* const kernel = f32 ? (rows == 8   ? &experts_down_few_kernel<true, 8>
+                                : rows == 4 ? &experts_down_few_kernel<true, 4>
+                                            : &experts_down_few_kernel<true, 2>)
+                             : (rows == 8   ? &experts_down_few_kernel<false, 8>
+                                : rows == 4 ? &experts_down_few_kernel<false, 4>
+                                            : &experts_down_few_kernel<false, 2>);
+    hipLaunchKernelGGL(kernel, grid, block, 0, s, a, expert_ids, params->first_expert, base, out, T);
     return hipGetLastError() == hipSuccess ? LASER_OK : LASER_E_LAUNCH;
   }
   const hipError_t err = f32 ? launch_products<true, false>(a, s) : launch_products<false, false>(a, s);
   if (err != hipSuccess) return LASER_E_LAUNCH;
   const size_t pieces = (size_t)T * (H / (f32 ? 4 : 8));
-  const unsigned grid = (unsigned)min((pieces + 255) / 256, (size_t)1 << 16);
+  const unsigned grid = (unsigned)std::min<size_t>((pieces + 255) / 256, 1 << 16);
   if (f32)
     hipLaunchKernelGGL((experts_combine_kernel<true>), dim3(grid), dim3(256), 0, s, workspace, nullptr, expert_ids, base, out,
                        T, H, params->k, params->first_expert, E);

@@ -113,9 +113,9 @@ struct Tile {
   __device__ static int piece(int wave, int lane) { return (lane & 7) ^ ((wave & 1) * 4 + (lane >> 4)); }
 
   // The product of one tile.  from[i]: where load i of this lane begins (row start + 16 *
-  // piece + kStepBytes * turn); `bytes`: length of the rows, a multiple of 16.  start() puts the first steps on
-  // their way to LDS, which nobody may be reading any more; run() does the rest and ends with
-  // every wavefront through with its reads of LDS.
+  // piece + kStepBytes * turn); `bytes`: length of the rows, a multiple of 16.  start() puts the
+  // first steps on their way to LDS, which nobody may be reading any more; run() does the rest and
+  // ends with every wavefront through with its reads of LDS.
   int steps, bytes;
   bool in_last;    // whether this lane's piece of the last step is inside the rows
   unsigned put;    // where this wavefront's loads go in slot 0
@@ -193,58 +193,42 @@ struct Tile {
     lds_barrier();
   }
 
-  // ST slots.  A step's operands are read while the step before is multiplied; with that its slot is
-  // free, and ST - 1 steps are on their way.
+  // ST slots.  A step's operands are read before the products of its first half: left to itself the
+  // compiler reads the second half behind them (16 tokens of 8 wide experts: 169 us instead of 166).
+  // With that a step's slot is free and loaded again while the products are made.  (Operands of the
+  // step after read ahead as well: no faster anywhere, and twice the registers for operands.)
   __device__ void run_ring(const unsigned char* (&from)[kLoads], int blocks, mma_f32x4 (&acc)[NB][MB]) {
-    mma_u32x4 w[2][2][NB], t[2][2][MB];  // [step % 2][half]
     unsigned slot = 0;
-    auto read = [&](int at) {
+    if (steps >= ST)
+      asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((ST - 1) * kLoads) : "memory");
+    else
+      asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+    for (int step = 0; step < steps; ++step) {
+      mma_u32x4 w[2][NB], t[2][MB];
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
 #pragma unroll
-        for (int n = 0; n < NB; ++n) w[at][s][n] = weight_block(slot, s, n);
+        for (int n = 0; n < NB; ++n) w[s][n] = weight_block(slot, s, n);
 #pragma unroll
         for (int m = 0; m < MB; ++m)
-          if (m < blocks) t[at][s][m] = token_block(slot, s, m);
+          if (m < blocks) t[s][m] = token_block(slot, s, m);
       }
-      __builtin_amdgcn_sched_barrier(0);  // (the compiler would put the reads behind the products)
-    };
-    auto products = [&](int at) {
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int s = 0; s < 2; ++s)
 #pragma unroll
         for (int m = 0; m < MB; ++m)
           if (m < blocks)
 #pragma unroll
-            for (int n = 0; n < NB; ++n) acc[n][m] = multiply<F32>(w[at][s][n], t[at][s][m], acc[n][m]);
-    };
-    // step + 1 is there, and everybody has read `step`, whose slot is loaded again
-    auto hand_over = [&](int step) {
+            for (int n = 0; n < NB; ++n) acc[n][m] = multiply<F32>(w[s][n], t[s][m], acc[n][m]);
+      if (step + 1 == steps) break;
+      // the next step is there, and everybody has read this one
       if (step + ST <= steps)
         asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((ST - 2) * kLoads) : "memory");
       else
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
       if (step + ST < steps) load_all(from, step + ST == steps - 1, slot);
       slot = slot == (ST - 1) * kStage ? 0 : slot + kStage;
-    };
-    if (steps >= ST)
-      asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((ST - 1) * kLoads) : "memory");
-    else
-      asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
-    read(0);
-    for (int step = 0; step < steps; step += 2) {
-      if (step + 1 < steps) {
-        hand_over(step);
-        read(1);
-      }
-      products(0);
-      if (step + 1 < steps) {
-        if (step + 2 < steps) {
-          hand_over(step + 1);
-          read(0);
-        }
-        products(1);
-      }
     }
   }
 
@@ -307,21 +291,21 @@ struct Tile {
   }
 };
 
-// Results -> memory by whole lines: a wavefront puts the blocks of its part of the tile into
-// a piece of LDS of its own (`lds`: the first of them; the second slot of two, or the whole ring), as many token blocks at a time as fit, and reads them back
-// row by row.  value(n, m): the four outputs of column block n < NC that this lane holds;
-// place(row, column): where the 16 bytes beginning at that row and (wavefront's) column go, or
-// NULL.  (Stores straight from the accumulators reach 16 rows with 32 or 64 bytes each:
+// Results -> memory by whole lines: a wavefront puts the blocks of its part of the tile into a
+// piece of LDS of its own (`lds`: the first of them; the second slot of two, or the whole ring), as
+// many token blocks at a time as fit, and reads them back row by row.  value(n, m): the four
+// outputs of column block n < NC that this lane holds; place(row, column): where the 16 bytes
+// beginning at that row and (wavefront's) column go, or NULL.  (Stores straight from the accumulators reach 16 rows with 32 or 64 bytes each:
 // 98304 x 2048 x 1408 in bf16 took 525 us so and 485 this way, with fp32 results 560 and 515,
 // with none 412.  They go past the caches: nobody reads them soon.)
 enum Stored { kF32, kBf16, kF16 };
 template <Stored AS, class TL, int NC, typename VALUE, typename PLACE>
 __device__ __forceinline__ void store_tile(unsigned lds, int wave, int lane, VALUE value, PLACE place) {
   constexpr int kBytes = TL::kStaging / TL::kWaves;
-  constexpr int kRow = NC * 16 * (AS == kF32 ? 4 : 2);                   // bytes of a row
+  constexpr int kRow = NC * 16 * (AS == kF32 ? 4 : 2);      // bytes of a row
   constexpr int kFit = kBytes / (16 * kRow);
-  constexpr int kPass = kFit < TL::MB ? kFit : TL::MB;             // token blocks at a time
-  constexpr int kPieces = kRow / 16, kRows = 64 / kPieces;         // pieces of a row; rows per store instruction
+  constexpr int kPass = kFit < TL::MB ? kFit : TL::MB;      // token blocks at a time
+  constexpr int kPieces = kRow / 16, kRows = 64 / kPieces;  // pieces of a row; rows per store instruction
   static_assert(kPass >= 1 && kPieces <= 16 && (kPieces & (kPieces - 1)) == 0, "whole instructions");
   const unsigned mine = lds + wave * kBytes;
   const int tok = lane & 15, quad = lane >> 4;
@@ -352,7 +336,9 @@ __device__ __forceinline__ void store_tile(unsigned lds, int wave, int lane, VAL
 #pragma unroll
     for (int i = 0; i < kStores; ++i) {
       const int r = i * kRows + lane / kPieces, c = lane % kPieces;
-      to[i] = r < kPass * 16 && m0 + r / 16 < TL::MB ? static_cast<mma_u32x4*>(place(TL::block_row(wave, m0 + r / 16) + r % 16, c * (AS == kF32 ? 4 : 8))) : nullptr;
+      const int row = TL::block_row(wave, m0 + r / 16) + r % 16;
+      const bool is = r < kPass * 16 && m0 + r / 16 < TL::MB;
+      to[i] = is ? static_cast<mma_u32x4*>(place(row, c * (AS == kF32 ? 4 : 8))) : nullptr;
       d[i] = read_lds(mine + min(r, kPass * 16 - 1) * kRow + (c ^ (r & kTurn)) * 16);
     }
 #pragma unroll

@@ -3,18 +3,21 @@
 //
 //   out[t, :] = W x_t + U_m (scale_m D_m x_t),   m the adapter of row t's request
 //
-// Two launches.  Of few rows and columns ("thin", see launch_project): sums over parts of the
-// contraction axis, of W and of the adapters side by side, then a join.  Else: the inner values
-// v = scale D x of all rows, then the shared product with U v added to its accumulators.
+// Where there is little to do side by side (see launch_project) the contraction axis is cut into
+// slices: one launch for sums over slices, of W and of the adapters' inner matrices alike, and one
+// that joins them.  Else: the inner values v = scale D x of all rows, then the shared product with U v
+// added to its accumulators; a gate's few columns do all of that in one launch.
 //
 // v stays in fp32 quality up to the second product: bf16 calls hand it over in three bf16 values
 // that add up to it (8 + 8 + 8 bits), each multiplied by U on its own.
+#include <algorithm>
+
 #include "../../include/laser.h"
 #include "grouped.h"
 
 namespace laser {
 
-constexpr int kThinSlices = 8;
+constexpr int kMostSlices = 8, kThinWaves = 4;
 
 struct ProjectArgs {
   const unsigned char* x;  // [T, K]
@@ -25,13 +28,15 @@ struct ProjectArgs {
   const int32_t* request_offsets;
   const int32_t* request_adapters;
   void* out;               // [T, N]
-  void* inner;             // v: [T, 3, R] bf16 or [T, R] fp32;  thin: [slices, T, R] fp32, not scaled
-  float* shared;           // thin: [slices, T, N];  more than one slice of tiles: v, [slices, T, R], not scaled
+  void* inner;             // v: [T, 3, R] bf16 or [T, R] fp32
+  float* parts;            // sums of slices: v, not scaled, [slices, T, R] ...
+  float* shared;           // ... and W x, [slices, T, N]
   int32_t* adapter;        // [T] the row's adapter, or -1
   int T, N, M, R, requests;
   int K;                   // bytes of a row of x, w and a_down
   int lanes;               // workgroups that share the distinct adapters of 16 rows
-  int slices;              // parts of the contraction axis (thin)
+  int slices;              // parts of the contraction axis
+  bool in_parts;           // v is left in sums of slices
 };
 
 // How many of request_offsets[0 .. requests - 1] are <= t; the same t in all lanes.
@@ -109,17 +114,17 @@ __device__ __forceinline__ void thin_product(const ThinTokens& head, const unsig
   }
 }
 
-// The WAVES wavefronts' sums of B blocks, added in their order; value i of a lane is row
+// The wavefronts' sums of B blocks, added in their order; value i of a lane is row
 // 4 (lane / 16) + i, token lane % 16.
-template <int B, int WAVES, typename USE>
+template <int B, typename USE>
 __device__ __forceinline__ void join_wavefronts(mma_f32x4 (&acc)[B], float* part, int wave, int lane, USE use) {
 #pragma unroll
-  for (int b = 0; b < B; ++b) *reinterpret_cast<mma_f32x4*>(part + ((b * WAVES + wave) * 64 + lane) * 4) = acc[b];
+  for (int b = 0; b < B; ++b) *reinterpret_cast<mma_f32x4*>(part + ((b * kThinWaves + wave) * 64 + lane) * 4) = acc[b];
   __syncthreads();
-  for (int b = wave; b < B; b += WAVES) {
-    mma_f32x4 sum = *reinterpret_cast<const mma_f32x4*>(part + (b * WAVES * 64 + lane) * 4);
+  for (int b = wave; b < B; b += kThinWaves) {
+    mma_f32x4 sum = *reinterpret_cast<const mma_f32x4*>(part + (b * kThinWaves * 64 + lane) * 4);
 #pragma unroll
-    for (int w = 1; w < WAVES; ++w) sum += *reinterpret_cast<const mma_f32x4*>(part + ((b * WAVES + w) * 64 + lane) * 4);
+    for (int w = 1; w < kThinWaves; ++w) sum += *reinterpret_cast<const mma_f32x4*>(part + ((b * kThinWaves + w) * 64 + lane) * 4);
     use(b, sum);
   }
   __syncthreads();
@@ -150,24 +155,24 @@ __device__ __forceinline__ void put_inner(const ProjectArgs& a, int t, int r, mm
   }
 }
 
-// Workgroup (x, y, z): 16 rows, every lanes-th of their distinct adapters from y on, slice z of
-// the contraction axis, cut over the wavefronts.  THIN: sums of slices, and behind the
-// first `lanes` y the shared projection, 16 columns each.
-template <bool F32, int B, bool THIN, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void adapter_inner_kernel(ProjectArgs a) {
-  __shared__ __align__(16) float part[B * WAVES * 256];
+// Thin calls.  Workgroup (x, y, z): 16 rows, every lanes-th of their distinct adapters from y on, slice z
+// of the contraction axis, cut over the wavefronts; behind the first `lanes` y the shared
+// projection, 16 columns each.
+template <bool F32, int B>
+__global__ __launch_bounds__(64 * kThinWaves) void adapter_thin_kernel(ProjectArgs a) {
+  __shared__ __align__(16) float part[B * kThinWaves * 256];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int t0 = blockIdx.x * 16, t = t0 + (lane & 15);
-  const int steps = (a.K + 63) >> 6, parts = WAVES * (THIN ? a.slices : 1), own = (THIN ? WAVES * (int)blockIdx.z : 0) + wave;
+  const int steps = (a.K + 63) >> 6, parts = kThinWaves * a.slices, own = kThinWaves * (int)blockIdx.z + wave;
   const int begin = (int)((long long)steps * own / parts), end = (int)((long long)steps * (own + 1) / parts);
   const unsigned char* const tokens = a.x + (size_t)min(t, a.T - 1) * a.K;
   const ThinTokens head(tokens, a.K, begin, end, lane);
-  if (THIN && (int)blockIdx.y >= a.lanes) {
+  if ((int)blockIdx.y >= a.lanes) {
     const int n0 = (blockIdx.y - a.lanes) * 16;
     const unsigned char* rows[1] = {a.w + (size_t)min(n0 + (lane & 15), a.N - 1) * a.K};
     mma_f32x4 acc[1] = {mma_f32x4{0.0f, 0.0f, 0.0f, 0.0f}};
     thin_product<F32, 1>(head, tokens, rows, a.K, begin, end, lane, acc);
-    join_wavefronts<1, WAVES>(acc, part, wave, lane, [&](int, mma_f32x4 sum) {
+    join_wavefronts<1>(acc, part, wave, lane, [&](int, mma_f32x4 sum) {
       if (t >= a.T) return;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -192,19 +197,14 @@ __global__ __launch_bounds__(64 * WAVES) void adapter_inner_kernel(ProjectArgs a
 #pragma unroll
     for (int b = 0; b < B; ++b) acc[b] = mma_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     thin_product<F32, B>(head, tokens, rows, a.K, begin, end, lane, acc);
-    const float scale = THIN || a.scales == nullptr ? 1.0f : a.scales[ad];
-    join_wavefronts<B, WAVES>(acc, part, wave, lane, [&](int b, mma_f32x4 sum) {
+    join_wavefronts<B>(acc, part, wave, lane, [&](int b, mma_f32x4 sum) {
       const int r = b * 16 + 4 * (lane >> 4);
-      if (!mine || r >= a.R) return;  // (R is a multiple of 4)
-      if constexpr (THIN)
-        store4<true>(a.inner, ((size_t)blockIdx.z * a.T + t) * a.R + r, sum);
-      else
-        put_inner<F32>(a, t, r, sum * scale);
+      if (mine && r < a.R) store4<true>(a.parts, ((size_t)blockIdx.z * a.T + t) * a.R + r, sum);  // (R: a multiple of 4)
     });
   }
 }
 
-// Thin calls, second launch: one workgroup per row and as many columns as it has threads.  All
+// The second launch of calls in slices: one workgroup per row and as many columns as it has threads.  All
 // that does not wait for another load is under way at once: the slices, the first 16 values of
 // the column's row of U.
 template <bool F32, bool OUT32>
@@ -212,13 +212,13 @@ __global__ __launch_bounds__(256) void adapter_join_kernel(ProjectArgs a) {
   __shared__ float v[LASER_MAX_RANK];
   const int t = blockIdx.x, n = blockIdx.y * blockDim.x + threadIdx.x, column = min(n, a.N - 1);
   const int m = a.adapter[t];
-  float part[kThinSlices];
+  float part[kMostSlices];
 #pragma unroll
-  for (int s = 0; s < kThinSlices; ++s)
+  for (int s = 0; s < kMostSlices; ++s)
     part[s] = s < a.slices ? a.shared[((size_t)s * a.T + t) * a.N + column] : 0.0f;
   float y = 0.0f;
 #pragma unroll
-  for (int s = 0; s < kThinSlices; ++s) y += part[s];
+  for (int s = 0; s < kMostSlices; ++s) y += part[s];
   if (m >= 0) {  // (the same for the whole workgroup)
     const size_t row = ((size_t)m * a.N + column) * a.R;
     mma_f32x4 u[4];
@@ -226,11 +226,11 @@ __global__ __launch_bounds__(256) void adapter_join_kernel(ProjectArgs a) {
     for (int i = 0; i < 4; ++i) u[i] = load4<F32>(a.a_up, row + min(4 * i, a.R - 4));
     for (int r = threadIdx.x; r < a.R; r += blockDim.x) {
 #pragma unroll
-      for (int s = 0; s < kThinSlices; ++s)
-        part[s] = s < a.slices ? static_cast<const float*>(a.inner)[((size_t)s * a.T + t) * a.R + r] : 0.0f;
+      for (int s = 0; s < kMostSlices; ++s)
+        part[s] = s < a.slices ? a.parts[((size_t)s * a.T + t) * a.R + r] : 0.0f;
       float sum = 0.0f;
 #pragma unroll
-      for (int s = 0; s < kThinSlices; ++s) sum += part[s];
+      for (int s = 0; s < kMostSlices; ++s) sum += part[s];
       v[r] = sum * (a.scales != nullptr ? a.scales[m] : 1.0f);
     }
     __syncthreads();
@@ -272,35 +272,46 @@ __global__ __launch_bounds__(512) void adapter_tiles_kernel(ProjectArgs a) {
   TL tile(end - begin, (unsigned)(size_t)(lds_bytes)ring, wave, lane);
   const int tok = lane & 15, quad = lane >> 4, wm = wave % 4, wn = wave / 4;
   const int t0 = blockIdx.x * 64;
-  if (wn == 0) {
-    const int m = adapter_of_row<16>(a, t0 + wm * 16, lane), t = t0 + wm * 16 + lane;
-    if (lane < 16) {
-      ids[wm * 16 + lane] = m;
-      if (t < a.T && slice == 0 && blockIdx.z == 0) a.adapter[t] = m;
+  const bool shared = (int)blockIdx.z >= a.lanes;  // rows of W instead of adapters'
+  const int n0 = ((int)blockIdx.z - a.lanes) * 128;
+  int id = -1, m = -1;
+  if (!shared) {
+    if (wn == 0) {
+      m = adapter_of_row<16>(a, t0 + wm * 16, lane);
+      const int t = t0 + wm * 16 + lane;
+      if (lane < 16) {
+        ids[wm * 16 + lane] = m;
+        if (t < a.T && slice == 0 && blockIdx.z == 0) a.adapter[t] = m;
+      }
     }
+    lds_barrier();
+    id = ids[lane];
+    m = ids[wm * 16 + tok];
   }
-  lds_barrier();
-  const int id = ids[lane], m = ids[wm * 16 + tok], t = t0 + wm * 16 + tok;
-  unsigned long long todo = __ballot(id >= 0);
+  const int t = t0 + wm * 16 + tok;
+  unsigned long long todo = shared ? 1 : __ballot(id >= 0);
   const unsigned char* from[TL::kLoads];
   for (int pass = 0; todo != 0; ++pass) {
     int held[kRoom];
 #pragma unroll
     for (int q = 0; q < kRoom; ++q) {
       held[q] = -1;
-      if (todo != 0) {
+      if (todo != 0 && !shared) {
         held[q] = __builtin_amdgcn_readlane(id, __builtin_ctzll(todo));
         todo &= ~__ballot(id == held[q]);
       }
     }
-    if (pass % a.lanes != (int)blockIdx.z) continue;
-    tile.turn_to(blockIdx.x);
+    if (shared) todo = 0;
+    else if (pass % a.lanes != (int)blockIdx.z) continue;
+    tile.turn_to(blockIdx.x + blockIdx.z);
     const int piece = TL::piece(wave, lane) * 16 + tile.turn * kStepBytes + begin;
 #pragma unroll
     for (int i = 0; i < TL::kLoads; ++i) {
       const int r = TL::row(wave, lane, i);
       if (r < 64) {
         from[i] = a.x + (size_t)min(t0 + r, a.T - 1) * a.K + piece;
+      } else if (shared) {
+        from[i] = a.w + (size_t)min(n0 + r - 64, a.N - 1) * a.K + piece;
       } else {
         const int x = r - 64, which = x / (16 * RB);  // (the same for all lanes of a load instruction)
         int ad = -1;
@@ -317,16 +328,23 @@ __global__ __launch_bounds__(512) void adapter_tiles_kernel(ProjectArgs a) {
     tile.run(from, 1, acc);
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
-      const int block = wn * 4 + n, r = block % RB * 16 + 4 * quad;
+      const int block = wn * 4 + n;
+      if (shared) {
+        const int c = n0 + block * 16 + 4 * quad;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (t < a.T && c + i < a.N) a.shared[((size_t)slice * a.T + t) * a.N + c + i] = acc[n][0][i];
+        continue;
+      }
+      const int r = block % RB * 16 + 4 * quad;
       int ad = -1;
 #pragma unroll
       for (int q = 0; q < kRoom; ++q) ad = block / RB == q ? held[q] : ad;
       if (ad < 0 || m != ad || r >= a.R) continue;
-      if (a.slices > 1) {
-        store4<true>(a.shared, ((size_t)slice * a.T + t) * a.R + r, acc[n][0]);
-      } else {
+      if (a.in_parts)
+        store4<true>(a.parts, ((size_t)slice * a.T + t) * a.R + r, acc[n][0]);
+      else
         put_inner<F32>(a, t, r, acc[n][0] * (a.scales != nullptr ? a.scales[ad] : 1.0f));
-      }
     }
   }
 }
@@ -339,14 +357,14 @@ __global__ __launch_bounds__(256) void adapter_slices_kernel(ProjectArgs a) {
   if (t >= a.T) return;
   const int m = a.adapter[t], r = (int)(i - t * quads) * 4;
   if (m < 0) return;
-  mma_f32x4 part[kThinSlices];
+  mma_f32x4 part[kMostSlices];
 #pragma unroll
-  for (int s = 0; s < kThinSlices; ++s)
-    part[s] = s < a.slices ? *reinterpret_cast<const mma_f32x4*>(a.shared + ((size_t)s * a.T + t) * a.R + r)
+  for (int s = 0; s < kMostSlices; ++s)
+    part[s] = s < a.slices ? *reinterpret_cast<const mma_f32x4*>(a.parts + ((size_t)s * a.T + t) * a.R + r)
                            : mma_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   mma_f32x4 sum = part[0];
 #pragma unroll
-  for (int s = 1; s < kThinSlices; ++s) sum += part[s];
+  for (int s = 1; s < kMostSlices; ++s) sum += part[s];
   put_inner<F32>(a, (int)t, r, sum * (a.scales != nullptr ? a.scales[m] : 1.0f));
 }
 
@@ -357,7 +375,7 @@ __device__ __forceinline__ void add_adapters(const ProjectArgs& a, int t0, int n
                                              mma_f32x4 (&acc)[TL::NB][TL::MB]) {
   constexpr int NB = TL::NB, MB = TL::MB, kPieces = F32 ? 1 : 3;
   constexpr int kSize = F32 ? 4 : 2, kOwn = 16 / kSize;  // values of v that a lane holds at a time
-  constexpr int kAhead = MB < 2 ? MB : 2;
+  constexpr int kAhead = MB <= 4 ? MB : 2;  // (registers)
   int ids[MB];
   bool any = false;
 #pragma unroll
@@ -635,26 +653,29 @@ __global__ __launch_bounds__(512) void project_narrow_kernel(ProjectArgs a) {
 
 // ---- host ---------------------------------------------------------------------------
 
+// Which way a call goes (launch_project), and what it keeps in the workspace.
 constexpr int kThinRows = 512, kThinValues = 1 << 16;
 static bool is_thin(int T, int N) { return T <= kThinRows && (long long)T * N <= kThinValues; }
+// slices so that `units` tiles become about as many workgroups as there are compute units
+constexpr int kWorkgroups = 256;
+static int slices_for(long long units, int K) {
+  const int steps = (K + kStepBytes - 1) / kStepBytes;
+  return (int)std::max<long long>(1, std::min<long long>({kMostSlices, kWorkgroups / units, steps}));
+}
 
 static size_t whole(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
-// Slices of the contraction axis of the inner values' tiles: workgroups for all compute units
-constexpr int kTileWorkgroups = 256;
-static int tile_slices(int T) { return max(1, min(kThinSlices, kTileWorkgroups / ((T + 63) / 64))); }
 struct ProjectLayout {
-  size_t adapter, inner, shared, total;
+  size_t adapter, inner, parts, shared, total;
 };
+// (each part grows with T.  Rows times slices, and values of out times slices, are at most those of kWorkgroups
+// tiles of 64 rows and of 64 x 128)
 static ProjectLayout project_layout(int T, int N, const laser_adapter_params_t* p) {
-  const bool thin = is_thin(T, N);
-  const size_t per_value = thin ? 4 * kThinSlices : p->dtype == LASER_DTYPE_F32 ? 4 : 6;
   ProjectLayout L;
   L.adapter = 0;
   L.inner = whole((size_t)T * 4);
-  L.shared = L.inner + whole((size_t)T * p->rank * per_value);
-  // (tiles: rows times slices, see tile_slices, at most; a size that grows with T)
-  const size_t sliced = T > kThinRows ? min((size_t)T * kThinSlices, (size_t)kTileWorkgroups * 64) : 0;
-  L.total = L.shared + 256 + whole(thin ? (size_t)T * N * 4 * kThinSlices : sliced * p->rank * 4);
+  L.parts = L.inner + whole((size_t)T * p->rank * (p->dtype == LASER_DTYPE_F32 ? 4 : 6));
+  L.shared = L.parts + whole(std::min<size_t>((size_t)T * kMostSlices, kWorkgroups * 64) * p->rank * 4);
+  L.total = L.shared + whole(std::min<size_t>((size_t)T * N * kMostSlices, kWorkgroups * 64 * 128) * 4) + 256;
   return L;
 }
 
@@ -672,18 +693,14 @@ static int check_project(int32_t T, int32_t H, int32_t N, const laser_adapter_pa
   return LASER_OK;
 }
 
-template <bool F32, bool THIN>
-static hipError_t launch_inner(const ProjectArgs& a, dim3 grid, hipStream_t s) {
-  // (thin calls have slices enough)
-  constexpr int kWaves = THIN ? 4 : 8;
-  if (a.R <= 16)
-    hipLaunchKernelGGL((adapter_inner_kernel<F32, 1, THIN, kWaves>), grid, dim3(64 * kWaves), 0, s, a);
-  else if (a.R <= 32)
-    hipLaunchKernelGGL((adapter_inner_kernel<F32, 2, THIN, kWaves>), grid, dim3(64 * kWaves), 0, s, a);
-  else if (a.R <= 64)
-    hipLaunchKernelGGL((adapter_inner_kernel<F32, 4, THIN, kWaves>), grid, dim3(64 * kWaves), 0, s, a);
-  else
-    hipLaunchKernelGGL((adapter_inner_kernel<F32, 8, THIN, kWaves>), grid, dim3(64 * kWaves), 0, s, a);
+template <bool F32>
+static hipError_t launch_thin(const ProjectArgs& a, hipStream_t s) {
+  const dim3 grid((a.T + 15) / 16, a.lanes + (a.N + 15) / 16, a.slices), block(64 * kThinWaves);
+  auto* const kernel = a.R <= 16   ? &adapter_thin_kernel<F32, 1>
+                       : a.R <= 32 ? &adapter_thin_kernel<F32, 2>
+                       : a.R <= 64 ? &adapter_thin_kernel<F32, 4>
+                                   : &adapter_thin_kernel<F32, 8>;
+  hipLaunchKernelGGL(kernel, grid, block, 0, s, a);
   return hipGetLastError();
 }
 
@@ -694,32 +711,29 @@ static hipError_t launch_tiles(const ProjectArgs& a, hipStream_t s) {
   hipError_t err = allow_dynamic_lds(fn, TL::kLdsBytes, attr);
   if (err != hipSuccess) return err;
   const long long grid = (long long)((a.T + TL::BM - 1) / TL::BM) * ((a.N + TL::BN - 1) / TL::BN);
-  hipLaunchKernelGGL((project_kernel<F32, OUT32, TL>), dim3((unsigned)min(grid, 1ll << 20)), dim3(TL::kThreads),
+  hipLaunchKernelGGL((project_kernel<F32, OUT32, TL>), dim3((unsigned)std::min(grid, 1ll << 20)), dim3(TL::kThreads),
                      TL::kLdsBytes, s, a);
   return hipGetLastError();
 }
 
-template <bool F32, bool OUT32>
-static hipError_t launch_shared(const ProjectArgs& a, hipStream_t s) {
-  if constexpr (!F32)
-    if ((long long)((a.T + 255) / 256) * ((a.N + 255) / 256) >= compute_units() / 2)
-      return launch_tiles<F32, OUT32, Tile<F32, 256, 256, 2, 4, 2>>(a, s);
-  return launch_tiles<F32, OUT32, Tile<F32, 64, 64, 1, 4, 4>>(a, s);
-}
-
 template <bool F32, int RB>
-static hipError_t launch_inner_tiles(const ProjectArgs& a, hipStream_t s) {
+static hipError_t launch_inner_tiles(const ProjectArgs& a, int columns, hipStream_t s) {
   static LdsAttr attr;
   constexpr int kLds = Tile<F32, 64, 128, 4, 2, 3>::kLdsBytes + 64 * 4;
   const void* fn = reinterpret_cast<const void*>(&adapter_tiles_kernel<F32, RB>);
-  hipError_t err = allow_dynamic_lds(fn, kLds, attr);
+  const hipError_t err = allow_dynamic_lds(fn, kLds, attr);
   if (err != hipSuccess) return err;
-  hipLaunchKernelGGL((adapter_tiles_kernel<F32, RB>), dim3((a.T + 63) / 64, a.slices, a.lanes), dim3(512), kLds, s, a);
-  err = hipGetLastError();
-  if (err != hipSuccess || a.slices == 1) return err;
-  const unsigned grid = (unsigned)(((long long)a.T * (a.R / 4) + 255) / 256);
-  hipLaunchKernelGGL((adapter_slices_kernel<F32>), dim3(grid), dim3(256), 0, s, a);
+  const dim3 grid((a.T + 63) / 64, a.slices, a.lanes + (columns + 127) / 128);
+  hipLaunchKernelGGL((adapter_tiles_kernel<F32, RB>), grid, dim3(512), kLds, s, a);
   return hipGetLastError();
+}
+// (columns: of the shared projection, 0 if they are not its business)
+template <bool F32>
+static hipError_t launch_inner(const ProjectArgs& a, int columns, hipStream_t s) {
+  return a.R <= 16   ? launch_inner_tiles<F32, 1>(a, columns, s)
+         : a.R <= 32 ? launch_inner_tiles<F32, 2>(a, columns, s)
+         : a.R <= 64 ? launch_inner_tiles<F32, 4>(a, columns, s)
+                     : launch_inner_tiles<F32, 8>(a, columns, s);
 }
 
 template <bool F32, bool OUT32, int RB>
@@ -729,43 +743,62 @@ static hipError_t launch_narrow(const ProjectArgs& a, hipStream_t s) {
   const void* fn = reinterpret_cast<const void*>(&project_narrow_kernel<F32, OUT32, RB>);
   hipError_t err = allow_dynamic_lds(fn, kLds, attr);
   if (err != hipSuccess) return err;
-  hipLaunchKernelGGL((project_narrow_kernel<F32, OUT32, RB>), dim3(min((a.T + 63) / 64, 1 << 20)), dim3(512), kLds, s, a);
+  hipLaunchKernelGGL((project_narrow_kernel<F32, OUT32, RB>), dim3(std::min((a.T + 63) / 64, 1 << 20)), dim3(512), kLds, s, a);
+  return hipGetLastError();
+}
+
+template <bool F32, bool OUT32>
+static hipError_t launch_join(const ProjectArgs& a, hipStream_t s) {
+  const int threads = a.N <= 64 ? 64 : a.N <= 128 ? 128 : 256;
+  hipLaunchKernelGGL((adapter_join_kernel<F32, OUT32>), dim3(a.T, (a.N + threads - 1) / threads), dim3(threads), 0, s, a);
   return hipGetLastError();
 }
 
 template <bool F32, bool OUT32>
 static hipError_t launch_project(ProjectArgs& a, hipStream_t s) {
-  const int rows16 = (a.T + 15) / 16;
   if (is_thin(a.T, a.N)) {
-    const int steps = (a.K + 63) / 64;
-    a.slices = min(kThinSlices, max(1, steps / 8));
-    a.lanes = a.requests > 0 ? min(16, a.requests) : 1;
-    hipError_t err = launch_inner<F32, true>(a, dim3(rows16, a.lanes + (a.N + 15) / 16, a.slices), s);
-    if (err != hipSuccess) return err;
-    const int threads = a.N <= 64 ? 64 : a.N <= 128 ? 128 : 256;
-    hipLaunchKernelGGL((adapter_join_kernel<F32, OUT32>), dim3(a.T, (a.N + threads - 1) / threads), dim3(threads), 0, s, a);
-    return hipGetLastError();
+    a.slices = std::min(kMostSlices, std::max(1, (a.K + 63) / 64 / 8));
+    a.lanes = std::max(1, std::min(16, a.requests));
+    const hipError_t err = launch_thin<F32>(a, s);
+    return err != hipSuccess ? err : launch_join<F32, OUT32>(a, s);
   }
   // (a tile of a gate makes its passes one after the other: not where many requests may meet in it)
   if (a.N <= kNarrowColumns && a.R <= kNarrowRank && (a.requests <= 32 || a.requests <= a.T / 64))
     return a.R <= 16   ? launch_narrow<F32, OUT32, 1>(a, s)
            : a.R <= 32 ? launch_narrow<F32, OUT32, 2>(a, s)
                        : launch_narrow<F32, OUT32, 4>(a, s);
-  if (a.T > kThinRows) {
-    a.slices = min(tile_slices(a.T), (a.K + kStepBytes - 1) / kStepBytes);
-    // (a tile's passes side by side; workgroups without one end at once.  Rank 128, 16384 rows of 40
-    // requests: 143 us with one, 126 with four)
-    a.lanes = max(1, min(a.requests, 4));
-    const hipError_t err = a.R <= 16 ? launch_inner_tiles<F32, 1>(a, s) : a.R <= 32 ? launch_inner_tiles<F32, 2>(a, s)
-                           : a.R <= 64 ? launch_inner_tiles<F32, 4>(a, s) : launch_inner_tiles<F32, 8>(a, s);
-    if (err != hipSuccess) return err;
-    return launch_shared<F32, OUT32>(a, s);
+  // (a tile's passes side by side; workgroups without one end at once.  Rank 128, 16384 rows of 40
+  // requests: 143 us with one, 126 with four)
+  a.lanes = std::max(1, std::min(a.requests, 4));
+  const long long rows = (a.T + 63) / 64, tiles = rows * ((a.N + 127) / 128);
+  // Too few tiles for half of the compute units: all in slices, unless the join would have more than
+  // kJoinWork products for single threads or there are few steps to cut.  (800 x 247, H = 3624: 67 us in
+  // tiles, 22 in slices; 1078 x 906, H = 640: 24, 27)
+  constexpr long long kJoinWork = 1 << 25;
+  constexpr int kJoinSteps = 16;
+  if (tiles + rows <= kWorkgroups / 2 && a.K >= kJoinSteps * kStepBytes && (long long)a.T * a.N * a.R <= kJoinWork) {
+    a.slices = slices_for(tiles + rows, a.K);
+    a.in_parts = true;
+    const hipError_t err = launch_inner<F32>(a, a.N, s);
+    return err != hipSuccess ? err : launch_join<F32, OUT32>(a, s);
   }
-  a.slices = 1;
-  a.lanes = a.requests > 0 ? min(min(16, a.requests), max(1, 1024 / rows16)) : 1;
-  hipError_t err = launch_inner<F32, false>(a, dim3(rows16, a.lanes, 1), s);
+  a.slices = slices_for(rows, a.K);
+  a.in_parts = a.slices > 1;
+  hipError_t err = launch_inner<F32>(a, 0, s);
   if (err != hipSuccess) return err;
-  return launch_shared<F32, OUT32>(a, s);
+  if (a.in_parts) {
+    const unsigned grid = (unsigned)(((long long)a.T * (a.R / 4) + 255) / 256);
+    hipLaunchKernelGGL((adapter_slices_kernel<F32>), dim3(grid), dim3(256), 0, s, a);
+    err = hipGetLastError();
+    if (err != hipSuccess) return err;
+  }
+  // tiles as large as leaves some for half of the compute units
+  auto count = [&](int side) { return (long long)((a.T + side - 1) / side) * ((a.N + side - 1) / side); };
+  if constexpr (!F32) {
+    if (count(256) >= kWorkgroups / 2) return launch_tiles<F32, OUT32, Tile<F32, 256, 256, 2, 4, 2>>(a, s);
+    if (count(128) >= kWorkgroups / 2) return launch_tiles<F32, OUT32, Tile<F32, 128, 128, 2, 2, 2>>(a, s);
+  }
+  return launch_tiles<F32, OUT32, Tile<F32, 64, 64, 1, 4, 4>>(a, s);
 }
 
 }  // namespace laser
@@ -774,9 +807,7 @@ using namespace laser;
 
 extern "C" size_t laser_project_workspace_bytes(int32_t T, int32_t H, int32_t N, const laser_adapter_params_t* params) {
   if (check_project(T, H, N, params) != LASER_OK) return 0;
-  // (a thin call may need more than one of more rows)
-  const int thin = min(T, min(kThinRows, kThinValues / N));
-  return max(project_layout(T, N, params).total, project_layout(thin, N, params).total);
+  return project_layout(T, N, params).total;
 }
 
 extern "C" int laser_project_adapted(const void* x, const void* w, int32_t T, int32_t H, int32_t N,
@@ -806,6 +837,7 @@ extern "C" int laser_project_adapted(const void* x, const void* w, int32_t T, in
   a.request_adapters = request_adapters;
   a.out = out;
   a.inner = ws + L.inner;
+  a.parts = reinterpret_cast<float*>(ws + L.parts);
   a.shared = reinterpret_cast<float*>(ws + L.shared);
   a.adapter = reinterpret_cast<int32_t*>(ws + L.adapter);
   a.T = T;
