@@ -29,7 +29,15 @@ SHAPES = [
     (300, 256, 64, 3, 2, 64, 61, 1.1),     # ... the last ones, hardly any row
     (1000, 136, 264, 7, 4, 9, 2, 0.5),
     (1500, 320, 392, 6, 3, 6, 0, 0.3),
-    (2600, 256, 272, 4, 2, 4, 0, 0.1),     # experts with rows for several of the widest tiles
+    (2600, 256, 272, 4, 2, 4, 0, 0.1),     # hundreds of rows per expert
+    (4, 312, 288, 13, 3, 21, 4, 0.0),      # the most tokens that go one by one, a share of the experts
+    (4, 64, 3000, 40, 16, 40, 0, 0.5),     # ... and the most slots
+    (5, 1032, 520, 4, 4, 4, 0, 0.0),
+    (1400, 1160, 136, 4, 2, 4, 0, 0.3),    # the widest tiles: rows of many steps, with a rest ...
+    (700, 136, 1208, 3, 2, 3, 0, 0.0),
+    (900, 1152, 1216, 2, 1, 2, 0, 1.0),    # ... and without
+    (1000, 1216, 1152, 4, 4, 32, 8, 0.0),  # a share with fewer rows than the tables hold for as many experts
+    (515, 2048, 1280, 1, 1, 1, 0, 0.0),
 ]
 
 

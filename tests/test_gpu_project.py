@@ -33,6 +33,8 @@ SHAPES = [
     (700, 264, 40, 64, 6, [1] * 70 + [5, 60, 65, 500]),              # many adapters in a tile of a gate
     (530, 1032, 200, 128, 40, [1] * 64 + [100, 3, 3, 300]),
     (2100, 328, 72, 16, 50, [1] * 130 + [2] * 20 + [1900]),
+    (2100, 264, 1100, 24, 5, [800, 0, 1299]),
+    (900, 1480, 240, 16, 3, [1, 898]),
     (900, 8, 96, 8, 3, [300, 300]),                                  # one step, no slices
     (1200, 136, 64, 48, 9, [400, 1, 1, 1, 797]),
     (4200, 200, 2061, 40, 6, [900, 20, 1, 2000, 1279]),              # the widest tiles, odd columns
