@@ -1,5 +1,6 @@
 // The experts of a layer over the routing tables: laser_experts_up and laser_experts_down.
 #include <algorithm>
+#include <type_traits>
 
 #include "../../include/laser.h"
 #include "grouped.h"
@@ -302,7 +303,9 @@ __device__ __forceinline__ float lanes_sum(float x) {  // in all lanes, one fixe
 }
 
 // sum[r] += row[r] times vector over the lane's pieces of chunks begin .. end - 1 (1 KiB each).
-template <bool F32, int ROWS, int BATCH>
+// ONCE: nobody reads the rows again, so they go past the caches.  One token (no expert twice): up
+// 16.9 -> 14.2 us, down 12.6 -> 11.7; four tokens of 8 experts: down 111 -> 132.
+template <bool F32, bool ONCE, int ROWS, int BATCH>
 __device__ __forceinline__ void row_products(const unsigned char* const (&row)[ROWS], const unsigned char* vector, int bytes,
                                              int begin, int end, int lane, float (&sum)[ROWS]) {
   for (int c = begin; c < end; c += BATCH) {
@@ -315,7 +318,8 @@ __device__ __forceinline__ void row_products(const unsigned char* const (&row)[R
       x[i] = *reinterpret_cast<const mma_u32x4*>(vector + from);
 #pragma unroll
       for (int r = 0; r < ROWS; ++r) {
-        w[i][r] = *reinterpret_cast<const mma_u32x4*>(row[r] + from);
+        w[i][r] = ONCE ? __builtin_nontemporal_load(reinterpret_cast<const mma_u32x4*>(row[r] + from))
+                       : *reinterpret_cast<const mma_u32x4*>(row[r] + from);
         if (!in) w[i][r] = mma_u32x4{0, 0, 0, 0};
       }
       if (!in) x[i] = mma_u32x4{0, 0, 0, 0};
@@ -333,28 +337,28 @@ __device__ __forceinline__ int expert_of(const ExpertTiles& t, int p) {
   return has == 0 ? -1 : __builtin_ctzll(has);
 }
 
-// blockIdx.x: the position; blockIdx.y: 4 wavefronts x kFewUp columns of act.
-constexpr int kFewUp = 2;
-template <bool F32>
+// blockIdx.x: the position; blockIdx.y: 4 wavefronts x COLUMNS columns of act (one token: 12.9 us with
+// one column, 14.2 with two; four tokens 42.8 and 42.3).
+template <bool F32, bool ONCE, int COLUMNS>
 __global__ __launch_bounds__(256) void experts_up_few_kernel(ExpertArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int p = blockIdx.x, f0 = (blockIdx.y * 4 + wave) * kFewUp;
+  const int p = blockIdx.x, f0 = (blockIdx.y * 4 + wave) * COLUMNS;
   ExpertTiles tiles;
   tiles.init(a, lane);
   const int e = expert_of(tiles, p);
   if (e < 0 || f0 >= a.F) return;
   const int t = a.permutation != nullptr ? min(max(a.permutation[p], 0), a.slots - 1) / a.k : p;
-  const unsigned char* row[2 * kFewUp];
+  const unsigned char* row[2 * COLUMNS];
 #pragma unroll
-  for (int i = 0; i < kFewUp; ++i) {
+  for (int i = 0; i < COLUMNS; ++i) {
     row[i] = a.w + ((size_t)e * 2 * a.F + min(f0 + i, a.F - 1)) * a.K;
-    row[kFewUp + i] = row[i] + (size_t)a.F * a.K;
+    row[COLUMNS + i] = row[i] + (size_t)a.F * a.K;
   }
-  float sum[2 * kFewUp] = {};
-  row_products<F32, 2 * kFewUp, 4>(row, a.x + (size_t)t * a.K, a.K, 0, (a.K + 1023) >> 10, lane, sum);
+  float sum[2 * COLUMNS] = {};
+  row_products<F32, ONCE, 2 * COLUMNS, 4>(row, a.x + (size_t)t * a.K, a.K, 0, (a.K + 1023) >> 10, lane, sum);
 #pragma unroll
-  for (int i = 0; i < kFewUp; ++i) {
-    const float y = silu<F32>(lanes_sum(sum[i])) * lanes_sum(sum[kFewUp + i]);
+  for (int i = 0; i < COLUMNS; ++i) {
+    const float y = silu<F32>(lanes_sum(sum[i])) * lanes_sum(sum[COLUMNS + i]);
     if (lane == 0 && f0 + i < a.F) {
       if constexpr (F32) static_cast<float*>(a.out)[(size_t)p * a.F + f0 + i] = y;
       else static_cast<unsigned short*>(a.out)[(size_t)p * a.F + f0 + i] = (unsigned short)bf16_bits(y);
@@ -362,12 +366,12 @@ __global__ __launch_bounds__(256) void experts_up_few_kernel(ExpertArgs a) {
   }
 }
 
-// ROWS rows of the matrices (columns of out) per workgroup, eight unless there are not enough for all
-// compute units.  Its wavefronts take the slots
+// ROWS rows of the matrices (columns of out) per workgroup, as many as leave two workgroups for every
+// compute unit (H = 2048, one token: eight rows 11.7 us, four 11.1; H = 128, three tokens: eight 26.8, two 19.4).  Its wavefronts take the slots
 // in turn, and where there are fewer slots than wavefronts, parts of the rows as well; what they
 // find waits in LDS for its place in the sums, which run in slot order.
 constexpr int kFewWaves = 8;
-template <bool F32, int ROWS>
+template <bool F32, bool ONCE, int ROWS>
 __global__ __launch_bounds__(64 * kFewWaves) void experts_down_few_kernel(ExpertArgs a, const int32_t* ids, int first,
                                                                           const void* base, void* out, int T) {
   __shared__ float found[kFewSlots * ROWS];
@@ -390,7 +394,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void experts_down_few_kernel(Expert
       const unsigned char* row[ROWS];
 #pragma unroll
       for (int r = 0; r < ROWS; ++r) row[r] = a.w + ((size_t)e * a.H + min(h0 + r, a.H - 1)) * a.K;
-      row_products<F32, ROWS, 3>(row, a.x + (size_t)p * a.K, a.K, chunks * part / parts, chunks * (part + 1) / parts,
+      row_products<F32, ONCE, ROWS, 3>(row, a.x + (size_t)p * a.K, a.K, chunks * part / parts, chunks * (part + 1) / parts,
                                      lane, sum);
     }
 #pragma unroll
@@ -417,12 +421,13 @@ __global__ __launch_bounds__(64 * kFewWaves) void experts_down_few_kernel(Expert
 }
 
 // out[t,:] = base[t,:] + the products of the token's slots that the call's experts hold, in
-// slot order.  One thread per 16 bytes of a slot's row; the rows of four slots are under way at a time.
+// slot order.  One thread per 16 bytes of a slot's row; the rows of kBatch slots are under way at a time.
 template <bool F32>
 __global__ __launch_bounds__(256) void experts_combine_kernel(const void* z, const float* factors, const int32_t* ids,
                                                               const void* base, void* out, int T, int H, int k, int first,
                                                               int E) {
   constexpr int kWide = F32 ? 4 : 8;  // columns of a thread
+  constexpr int kBatch = 4;
   const int pieces = H / kWide, blocks = shared_blocks(H);
   const size_t all = (size_t)T * pieces;
   for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (size_t)gridDim.x * 256) {
@@ -434,15 +439,15 @@ __global__ __launch_bounds__(256) void experts_combine_kernel(const void* z, con
       y[q] = mma_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
       if (base != nullptr) y[q] = load4<F32>(base, t * H + h + 4 * q);
     }
-    for (int j = 0; j < k; j += 4) {
-      mma_u32x4 row[4];
-      float by[4];
-      bool is[4];
+    for (int j = 0; j < k; j += kBatch) {
+      mma_u32x4 row[kBatch];
+      float by[kBatch];
+      bool is[kBatch];
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
+      for (int u = 0; u < kBatch; ++u)
         is[u] = j + u < k && (ids == nullptr || (unsigned)(ids[t * k + min(j + u, k - 1)] - first) < (unsigned)E);
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
+      for (int u = 0; u < kBatch; ++u) {
         const size_t slot = t * k + j + u;
         if (is[u]) {
           row[u] = __builtin_nontemporal_load(
@@ -451,7 +456,7 @@ __global__ __launch_bounds__(256) void experts_combine_kernel(const void* z, con
         }
       }
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
+      for (int u = 0; u < kBatch; ++u) {
         if (!is[u]) continue;
         if constexpr (F32) {
           y[0] += __builtin_bit_cast(mma_f32x4, row[u]);
@@ -579,11 +584,11 @@ extern "C" int laser_experts_up(const void* hidden, const void* w_up, int32_t T,
   clear_stale_error();
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   if (are_few(T, a.slots, F)) {
-    const dim3 grid(a.slots, (F + 4 * kFewUp - 1) / (4 * kFewUp));
-    if (f32)
-      hipLaunchKernelGGL((experts_up_few_kernel<true>), grid, dim3(256), 0, s, a);
-    else
-      hipLaunchKernelGGL((experts_up_few_kernel<false>), grid, dim3(256), 0, s, a);
+    const int columns = T == 1 ? 1 : 2;
+    const dim3 grid(a.slots, (F + 4 * columns - 1) / (4 * columns));
+    auto* const kernel = f32 ? (T == 1 ? &experts_up_few_kernel<true, true, 1> : &experts_up_few_kernel<true, false, 2>)
+                             : (T == 1 ? &experts_up_few_kernel<false, true, 1> : &experts_up_few_kernel<false, false, 2>);
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a);
     return hipGetLastError() == hipSuccess ? LASER_OK : LASER_E_LAUNCH;
   }
   const hipError_t err = f32 ? launch_products<true, true>(a, s) : launch_products<false, true>(a, s);
@@ -630,14 +635,16 @@ extern "C" int laser_experts_down(const void* act, const void* w_down, int32_t T
   clear_stale_error();
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   if (are_few(T, a.slots, F)) {
-    const int rows = H >= 8 * compute_units() ? 8 : H >= 4 * compute_units() ? 4 : 2;
+    const int rows = H >= 16 * compute_units() ? 8 : H >= 8 * compute_units() ? 4 : 2;
     const dim3 grid((H + rows - 1) / rows), block(64 * kFewWaves);
-    auto* const kernel = f32 ? (rows == 8   ? &experts_down_few_kernel<true, 8>
-                                : rows == 4 ? &experts_down_few_kernel<true, 4>
-                                            : &experts_down_few_kernel<true, 2>)
-                             : (rows == 8   ? &experts_down_few_kernel<false, 8>
-                                : rows == 4 ? &experts_down_few_kernel<false, 4>
-                                            : &experts_down_few_kernel<false, 2>);
+    auto pick = [&](auto is32, auto once) {
+      constexpr bool k32 = decltype(is32)::value, kOnce = decltype(once)::value;
+      return rows == 8   ? &experts_down_few_kernel<k32, kOnce, 8>
+             : rows == 4 ? &experts_down_few_kernel<k32, kOnce, 4>
+                         : &experts_down_few_kernel<k32, kOnce, 2>;
+    };
+    auto* const kernel = f32 ? (T == 1 ? pick(std::true_type{}, std::true_type{}) : pick(std::true_type{}, std::false_type{}))
+                             : (T == 1 ? pick(std::false_type{}, std::true_type{}) : pick(std::false_type{}, std::false_type{}));
     hipLaunchKernelGGL(kernel, grid, block, 0, s, a, expert_ids, params->first_expert, base, out, T);
     return hipGetLastError() == hipSuccess ? LASER_OK : LASER_E_LAUNCH;
   }
