@@ -513,7 +513,9 @@ static hipError_t launch_experts(const ExpertArgs& a, int rows, long long most, 
 constexpr int kSomeRows = 96, kManyRows = 160, kWideSteps = 18;
 template <bool F32, bool UP>
 static hipError_t launch_products(const ExpertArgs& a, hipStream_t s) {
-  using LOW = Tile<F32, 64, 128, 2, 2, 3>;
+  // (most experts then have one tile of rows, so their weights are read once: 64 tokens on 64 experts 128 us,
+  // past the caches 114; 16 on 8 wide ones 162, 145.  With 128 x 128 it is the other way round: 200, 211)
+  using LOW = Tile<F32, 64, 128, 2, 2, 3, F32 ? kNeither : kWeights>;
   if constexpr (F32) {
     if (grid_of<LOW, UP>(a) < compute_units())
       return launch_experts<F32, UP, Tile<F32, 32, 64, 2, 2, 6>, false>(a, 0, kGridMost, s);
@@ -541,7 +543,7 @@ static int check_experts(int32_t T, int32_t H, int32_t F, int32_t E, const laser
 }
 
 // (F: a dimension of the grid)
-static bool are_few(int T, int slots, int F) { return T <= kFewTokens && slots <= kFewSlots && F <= 1 << 18; }
+static bool are_few(int T, int slots, int F) { return T <= kFewTokens && slots <= kFewSlots && F <= 1 << 17; }
 
 static size_t whole_256(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
 static bool misaligned(const void* p) { return ((uintptr_t)p & 15) != 0; }

@@ -40,9 +40,11 @@ struct false_c {
 static __device__ __align__(16) const unsigned int zero_piece[4] = {0, 0, 0, 0};
 
 // 64 x 16 bytes, lane l's to LDS byte `lds` + 16 l.  Only vmcnt says when they are there.
+// (ONCE: past the caches)
+template <bool ONCE>
 __device__ __forceinline__ void load_to_lds(const unsigned char* from, unsigned lds) {
   __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
-                                   (__attribute__((address_space(3))) void*)(size_t)lds, 16, 0, 0);
+                                   (__attribute__((address_space(3))) void*)(size_t)lds, 16, 0, ONCE ? 2 : 0);
 }
 
 __device__ __forceinline__ mma_u32x4 read_lds(unsigned at) { return *(lds_piece)(size_t)at; }
@@ -94,8 +96,10 @@ __device__ __forceinline__ mma_f32x4 load4(const void* row, size_t at) {
   }
 }
 
-// WM x WN wavefronts, each with (BM / WM) x (BN / WN) of the tile.
-template <bool F32, int BM_, int BN_, int WM_, int WN_, int ST_>
+// WM x WN wavefronts, each with (BM / WM) x (BN / WN) of the tile.  ONCE: the operand that nobody else
+// reads.
+enum Operand { kNeither, kTokens, kWeights };
+template <bool F32, int BM_, int BN_, int WM_, int WN_, int ST_, Operand ONCE = kNeither>
 struct Tile {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, ST = ST_;
   static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
@@ -151,7 +155,11 @@ struct Tile {
     const unsigned char* p = from[i];
     from[i] += by;
     if (last) p = in_last ? p : reinterpret_cast<const unsigned char*>(zero_piece);
-    load_to_lds(p, put + slot + i * kWaves * 8 * kStepBytes);
+    // (which operand load i brings is known here where no load brings both)
+    if (BM % (8 * kWaves) == 0 && ONCE == (i < BM / (8 * kWaves) ? kTokens : kWeights))
+      load_to_lds<true>(p, put + slot + i * kWaves * 8 * kStepBytes);
+    else
+      load_to_lds<false>(p, put + slot + i * kWaves * 8 * kStepBytes);
   }
   template <typename LAST>
   __device__ void load_all(const unsigned char* (&from)[kLoads], LAST last, unsigned slot) {

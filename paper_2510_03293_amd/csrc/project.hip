@@ -517,7 +517,7 @@ __global__ __launch_bounds__(TL::kThreads) void project_kernel(ProjectArgs a) {
 constexpr int kNarrowColumns = 64, kNarrowRank = 64;
 template <bool F32, bool OUT32, int RB>  // RB: blocks of 16 that hold an adapter's rows
 __global__ __launch_bounds__(512) void project_narrow_kernel(ProjectArgs a) {
-  using TL = Tile<F32, 64, 128, 4, 2, 6>;
+  using TL = Tile<F32, 64, 128, 4, 2, 6, kTokens>;
   constexpr int kRoom = 4 / RB;  // adapters beside W, twice that without
   extern __shared__ __align__(1024) unsigned char ring[];
   int* const ids = reinterpret_cast<int*>(ring + TL::kLdsBytes);
