@@ -254,18 +254,46 @@ __device__ __forceinline__ void experts_tiles(const ExpertArgs& a, unsigned char
   }
 }
 
-// How many rows the call's experts have is known on the device only: a call that may have either
-// many or few per expert (`rows`: the number from which they are many, 0: no question) is launched
-// with wide tiles and with narrow ones, and one of the two launches finds that it is not meant.
-template <bool F32, bool UP, class TL, bool MANY>
-__global__ __launch_bounds__(TL::kThreads) void experts_kernel(ExpertArgs a, int rows) {
+// How many rows the call's experts have, and how they fill tiles, is known on the device only: a call
+// that wide tiles may suit is launched with wide ones and with others, and one of the two
+// launches finds that it is not meant.
+//
+// What the two would take, in twentieths of a microsecond: as many rounds of tiles as workgroups run
+// side by side, of so much per step and so much before and behind the steps (fitted to the figures
+// below; of a compute unit's two workgroups with 128 x 128 each has half of the steps' rate).
+//   us with 128 x 128, 256 x 256:  up of H = 2048, F = 1408, 64 experts, 2048 tokens 248, 230, 4096 tokens 390, 327;
+//   down of the same 162, 166 and 274, 240;  16 of the 64 experts, 1501 tokens, 2600 rows 27, 42;  up of H = 4096,
+//   F = 2048, 8 experts, 1024 tokens 141, 109;  down of F = 4096, H = 4096, 8 experts, 1500 tokens 147, 164
+struct Wide {
+  using TL = Tile<false, 256, 256, 2, 4, 2>;
+  static constexpr int kPerCu = 1, kStep = 25, kTile = 120, kOnce = 120;
+};
+struct Medium {
+  using TL = Tile<false, 128, 128, 2, 2, 2>;
+  static constexpr int kPerCu = 2, kStep = 19, kTile = 120, kOnce = 0;
+};
+template <class HOW, bool UP>
+__device__ __forceinline__ long long cost_of(const ExpertArgs& a, ExpertTiles& tiles, int lane, unsigned units) {
+  tiles.count(lane, HOW::TL::BM);
+  constexpr int kCols = UP ? HOW::TL::BN / 2 : HOW::TL::BN;
+  const long long all = (long long)tiles.total * (((UP ? a.F : a.H) + kCols - 1) / kCols);
+  // (a division in 64 bits would take longer than the rest)
+  const unsigned most = (unsigned)(all < (1 << 30) ? all : (1 << 30));
+  const unsigned rounds = (most + HOW::kPerCu * units - 1) / (HOW::kPerCu * units);
+  // (in integers: the two launches have to come to the same)
+  return (long long)rounds * (HOW::kStep * ((a.K + kStepBytes - 1) / kStepBytes) + HOW::kTile) + HOW::kOnce;
+}
+
+enum Choose { kSure, kIfWide, kIfMedium };
+template <bool F32, bool UP, class TL, Choose WHEN>
+__global__ __launch_bounds__(TL::kThreads) void experts_kernel(ExpertArgs a, unsigned units) {
   extern __shared__ __align__(1024) unsigned char ring[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   ExpertTiles tiles;
   tiles.init(a, lane);
-  if (rows != 0) {
-    tiles.count(lane, 1);
-    if ((tiles.total >= (long long)rows * a.E) != MANY) return;
+  if constexpr (WHEN != kSure) {
+    const bool wide = cost_of<Wide, UP>(a, tiles, lane, units) <= cost_of<Medium, UP>(a, tiles, lane, units);
+    if (wide != (WHEN == kIfWide)) return;
   }
   experts_tiles<F32, UP, TL>(a, ring, tiles, lane, wave);
 }
@@ -486,31 +514,27 @@ static long long grid_of(const ExpertArgs& a) {
   return mt * (((UP ? a.F : a.H) + cols - 1) / cols);
 }
 
-template <bool F32, bool UP, class TL, bool MANY>
-static hipError_t launch_experts(const ExpertArgs& a, int rows, long long most, hipStream_t s) {
+template <bool F32, bool UP, class TL, Choose WHEN>
+static hipError_t launch_experts(const ExpertArgs& a, long long most, hipStream_t s) {
   static LdsAttr attr;
-  const void* fn = reinterpret_cast<const void*>(&experts_kernel<F32, UP, TL, MANY>);
+  const void* fn = reinterpret_cast<const void*>(&experts_kernel<F32, UP, TL, WHEN>);
   hipError_t err = allow_dynamic_lds(fn, lds_of<TL>(), attr);
   if (err != hipSuccess) return err;
   const unsigned grid = (unsigned)std::min(grid_of<TL, UP>(a), most);
-  hipLaunchKernelGGL((experts_kernel<F32, UP, TL, MANY>), dim3(grid), dim3(TL::kThreads), lds_of<TL>(), s, a, rows);
+  hipLaunchKernelGGL((experts_kernel<F32, UP, TL, WHEN>), dim3(grid), dim3(TL::kThreads), lds_of<TL>(), s, a,
+                     (unsigned)compute_units());
   return hipGetLastError();
 }
 
-// Which tiles.  bf16, by the rows per expert (us for H = 2048, F = 1408, 64 experts; tiles of
-// 64 x 128, 128 x 128 and 256 x 256):
-//   up:    48 rows on average 167, 182, -;   192 rows 304, 248, 230;   384 rows 514, 390, 327
-//   down:  48 rows 102, 110, -;              192 rows 198, 162, 166;   384 rows 338, 274, 240
-// The host knows the rows per expert if they were even, an upper bound where the call's experts are a
-// share of the layer's: only above kSomeRows are both of the larger tiles launched, with kManyRows
-// between them.  fp32 is bound by its matrix instructions (a sixteenth of the rate) as soon as there
-// are tiles for all compute units; before that, small tiles are more of them (333 tokens, 33
-// experts, 516 x 212: 30 us with tiles of 64 x 128, 20 with 32 x 64; 4000 tokens, 8 experts,
-// 1024 x 1024: 333 and 391).
-// With few steps what comes before and behind them counts, of which two workgroups of a compute unit
-// hide each other's (8000 tokens, 2000 rows per expert, 128 x 128 and 256 x 256: down of F = 320 70, 76,
-// F = 1024 109, 116; up of H = 136 62, 80, H = 640 103, 102, H = 1024 145, 141).
-constexpr int kSomeRows = 96, kManyRows = 160, kWideSteps = 18;
+// Which tiles.  bf16, by the rows per expert if they were even, of which the host knows an upper bound
+// (the call's experts may be a share of the layer's): few, 64 x 128 (48 rows per expert of H = 2048, F = 1408: up
+// 167 us, with 128 x 128 182; 192 rows: 304, 248); more, what cost_of says, unless the rows have so few
+// steps that 256 x 256 cannot win (8000 tokens, 2000 rows per expert, 128 x 128 and 256 x 256: down of F = 320 70,
+// 76, F = 1024 109, 116; up of H = 136 62, 80, H = 640 103, 102, H = 1024 145, 141).
+// fp32 is bound by its matrix instructions (a sixteenth of the rate) as soon as there are tiles for
+// all compute units; before that, small tiles are more of them (333 tokens, 33 experts, 516 x 212: 30 us
+// with tiles of 64 x 128, 20 with 32 x 64; 4000 tokens, 8 experts, 1024 x 1024: 333 and 391).
+constexpr int kSomeRows = 96, kWideSteps = 18;
 template <bool F32, bool UP>
 static hipError_t launch_products(const ExpertArgs& a, hipStream_t s) {
   // (most experts then have one tile of rows, so their weights are read once: 64 tokens on 64 experts 128 us,
@@ -518,16 +542,14 @@ static hipError_t launch_products(const ExpertArgs& a, hipStream_t s) {
   using LOW = Tile<F32, 64, 128, 2, 2, 3, F32 ? kNeither : kWeights>;
   if constexpr (F32) {
     if (grid_of<LOW, UP>(a) < compute_units())
-      return launch_experts<F32, UP, Tile<F32, 32, 64, 2, 2, 6>, false>(a, 0, kGridMost, s);
+      return launch_experts<F32, UP, Tile<F32, 32, 64, 2, 2, 6>, kSure>(a, kGridMost, s);
   } else if (a.slots >= (long long)kSomeRows * a.E) {
-    const bool wide = a.slots >= kManyRows && a.K >= kWideSteps * kStepBytes;
-    if (wide) {
-      const hipError_t err = launch_experts<F32, UP, Tile<F32, 256, 256, 2, 4, 2>, true>(a, kManyRows, compute_units(), s);
-      if (err != hipSuccess) return err;
-    }
-    return launch_experts<F32, UP, Tile<F32, 128, 128, 2, 2, 2>, false>(a, wide ? kManyRows : 0, 4 * compute_units(), s);
+    const long long most = Medium::kPerCu * 2 * compute_units();
+    if (a.K < kWideSteps * kStepBytes) return launch_experts<F32, UP, Medium::TL, kSure>(a, most, s);
+    const hipError_t err = launch_experts<F32, UP, Wide::TL, kIfWide>(a, Wide::kPerCu * compute_units(), s);
+    return err != hipSuccess ? err : launch_experts<F32, UP, Medium::TL, kIfMedium>(a, most, s);
   }
-  return launch_experts<F32, UP, LOW, false>(a, 0, kGridMost, s);
+  return launch_experts<F32, UP, LOW, kSure>(a, kGridMost, s);
 }
 
 static int check_experts(int32_t T, int32_t H, int32_t F, int32_t E, const laser_experts_params_t* p) {
