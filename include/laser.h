@@ -8,6 +8,10 @@
  * advance after every token, and the token-to-expert dispatch tables.
  * (Paper: section "The Method" -- Problem Formulation, Expansion rule, Final
  * assignment; appendix "Pseudo Code", Algorithm 1 "per token, per layer".)
+ * Further calls do what a layer needs beside that step: the experts' products over the
+ * dispatch tables (laser_experts_up, laser_experts_down), and a gate, or any other
+ * projection, whose requests bring low-rank adapters of their own
+ * (laser_project_adapted).
  *
  * Conventions
  *   - Every data pointer is a DEVICE pointer unless marked host.  The caller
@@ -62,10 +66,10 @@ extern "C" {
 
 #define LASER_OK 0
 #define LASER_E_NULL (-1)        /* a required pointer is NULL                    */
-#define LASER_E_RANGE (-2)       /* T, H, E, k, c, eps_high or t_fix out of range */
+#define LASER_E_RANGE (-2)       /* a size or a parameter out of range             */
 #define LASER_E_ALIGN (-3)       /* row length or pointer alignment not supported */
-#define LASER_E_WORKSPACE (-4)   /* workspace smaller than laser_workspace_bytes  */
-#define LASER_E_UNSUPPORTED (-5) /* E or c above the built limit                  */
+#define LASER_E_WORKSPACE (-4)   /* workspace smaller than its query says         */
+#define LASER_E_UNSUPPORTED (-5) /* E, k, c or rank above the built limit         */
 #define LASER_E_STRUCT (-6)      /* params->struct_bytes does not match           */
 #define LASER_E_LAUNCH (-7)      /* the HIP runtime refused a kernel launch       */
 
@@ -355,7 +359,7 @@ size_t laser_project_workspace_bytes(int32_t T, int32_t H, int32_t N,
  *   workspace        >= laser_project_workspace_bytes(...) bytes, 256-byte aligned
  * a_down, a_up, request_offsets and request_adapters may be NULL if there are no adapters
  * or no requests.  H a multiple of 8 (bf16) or 4 (fp32), matrices 16-byte aligned and
- * without gaps between rows; N is free; T <= 2^27.
+ * without gaps between rows; N is free; T <= 2^27, requests <= 2^28.
  */
 int laser_project_adapted(const void* x, const void* w, int32_t T, int32_t H, int32_t N,
                           const laser_adapter_params_t* params, const void* a_down,

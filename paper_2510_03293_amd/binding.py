@@ -6,6 +6,7 @@ fallback: if the library has not been built, importing the binding raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -446,10 +447,20 @@ def _expect(name: str, t, shape, dtype, device, optional: bool = False) -> None:
         raise ValueError(f"{name} must be contiguous")
 
 
-def _expect_current(device) -> None:
-    """The library launches on the current device, so that is where the tensors have to be."""
+def _expect_current(device, stream, workspace=None) -> None:
+    """The library launches on the current device, so that is where the tensors and the stream have to be."""
     if device.type != "cuda" or device.index != torch.cuda.current_device():
         raise ValueError(f"tensors are on {device}: they must be on the current GPU")
+    if stream is not None and stream.device != device:
+        raise ValueError(f"the stream belongs to {stream.device}, not to {device}")
+    if workspace is not None and (workspace.device != device or not workspace.is_contiguous()):
+        raise ValueError(f"buffers.workspace must be contiguous and on {device}")
+
+
+def _memory_of(stream):
+    """Where a call allocates what it works in: memory of the call's own stream, which neither earlier
+    work of the current stream uses any more nor later work of it gets while the call runs."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
 
 
 class ExpertBuffers:
@@ -470,7 +481,7 @@ def experts(hidden, w_up, w_down, routed: RouteBuffers | None, base=None, first_
             buffers: ExpertBuffers | None = None, stream=None) -> ExpertBuffers:
     """Both products of the experts behind a routing call: laser_experts_up, then laser_experts_down
     with the call's weights.  w_up [E,2F,H], w_down [E,H,F]; routed None: one expert (E = 1) for every
-    token.  The result is `out` of the returned buffers."""
+    token.  The result is `out` of the returned buffers; forward only."""
     code = _dtype_code(hidden, "hidden")
     if hidden.dim() != 2 or w_down.dim() != 3:
         raise ValueError("hidden must have 2 dimensions, w_down 3")
@@ -491,9 +502,10 @@ def experts(hidden, w_up, w_down, routed: RouteBuffers | None, base=None, first_
     if buffers is not None:
         _expect("buffers.act", buffers.act, (T * k, F), dt, dev)
         _expect("buffers.out", buffers.out, (T, H), dt, dev)
-    _expect_current(dev)
+    _expect_current(dev, stream, None if buffers is None else buffers.workspace)
     if buffers is None:
-        buffers = ExpertBuffers(T, H, F, E, k, dt, device=dev)
+        with _memory_of(stream):
+            buffers = ExpertBuffers(T, H, F, E, k, dt, device=dev)
     params = make_experts_params(k, code, first_expert)
     tables = (None,) * 4 if routed is None else (routed.permutation, routed.expert_offsets, routed.expert_ids,
                                                  routed.weights)
@@ -518,7 +530,7 @@ def project_adapted(x, w, a_down, a_up, scales, request_offsets, request_adapter
                     buffers: ProjectBuffers | None = None, stream=None) -> torch.Tensor:
     """laser_project_adapted with sizes from the tensors: x [T,H], w [N,H], a_down [M,R,H], a_up [M,N,R],
     scales [M] fp32 or None, request_offsets [requests+1] and request_adapters [requests] int32.
-    out_dtype: that of x (default) or float32.  Returns out [T,N]."""
+    out_dtype: that of x (default) or float32.  Returns out [T,N]; forward only."""
     code = _dtype_code(x, "x")
     if x.dim() != 2 or w.dim() != 2 or a_down.dim() != 3 or request_adapters.dim() != 1:
         raise ValueError("x and w must have 2 dimensions, a_down 3, request_adapters 1")
@@ -535,10 +547,11 @@ def project_adapted(x, w, a_down, a_up, scales, request_offsets, request_adapter
     _expect("request_adapters", request_adapters, (n,), torch.int32, dev)
     if buffers is not None:
         _expect("buffers.out", buffers.out, (T, N), out_dtype, dev)
-    _expect_current(dev)
+    _expect_current(dev, stream, None if buffers is None else buffers.workspace)
     params = make_adapter_params(R, M, n, code, _CODES[out_dtype])
     if buffers is None:
-        buffers = ProjectBuffers(T, H, N, params, device=dev)
+        with _memory_of(stream):
+            buffers = ProjectBuffers(T, H, N, params, device=dev)
     laser_project_adapted(x, w, T, H, N, params, a_down, a_up, scales, request_offsets, request_adapters,
                           buffers.out, buffers.workspace, stream)
     return buffers.out

@@ -449,11 +449,11 @@ const char* laser_strerror(int code) {
   switch (code) {
     case LASER_OK: return "ok";
     case LASER_E_NULL: return "a required pointer is NULL";
-    case LASER_E_RANGE: return "argument out of range (B, T, H, E, k, c, eps_high, t_fix or dtype)";
+    case LASER_E_RANGE: return "argument out of range (B, T, H, F, N, E, k, c, eps_high, t_fix, rank, adapters, requests or dtype)";
     case LASER_E_ALIGN: return "unsupported row length or pointer alignment";
     case LASER_E_WORKSPACE: return "workspace too small";
-    case LASER_E_UNSUPPORTED: return "not built: E > 64 or k > 16";
-    case LASER_E_STRUCT: return "laser_params_t.struct_bytes mismatch";
+    case LASER_E_UNSUPPORTED: return "not built: E > 64, k > 16 or rank > 128";
+    case LASER_E_STRUCT: return "struct_bytes of the parameters mismatch";
     case LASER_E_LAUNCH: return "a HIP call failed (kernel launch, event, copy)";
     default: return "unknown error code";
   }

@@ -59,7 +59,7 @@ struct ExpertTiles {
     }
   }
   __device__ void count(int lane, int BM) {
-    const int tiles = (cnt + BM - 1) / BM;
+    const int tiles = (int)(((unsigned)cnt + BM - 1) / BM);
     int sum = tiles;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -74,7 +74,7 @@ struct ExpertTiles {
   __device__ void find(int id, int nt, int BM, int& e, int& p0, int& rows, int& column) const {
     constexpr int kGroup = 8;
     e = 63 - __builtin_clzll(__ballot(cnt > 0 && before <= id / nt));
-    const int n = __builtin_amdgcn_readlane(cnt, e), mts = (n + BM - 1) / BM;
+    const int n = __builtin_amdgcn_readlane(cnt, e), mts = (int)(((unsigned)n + BM - 1) / BM);
     const int in_e = id - __builtin_amdgcn_readlane(before, e) * nt;
     const int g = in_e / (kGroup * nt), gm = min(kGroup, mts - g * kGroup), in = in_e - g * kGroup * nt;
     column = in / gm;

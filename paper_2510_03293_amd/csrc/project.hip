@@ -685,7 +685,7 @@ static int check_project(int32_t T, int32_t H, int32_t N, const laser_adapter_pa
   if (!p) return LASER_E_NULL;
   if (p->struct_bytes != sizeof(laser_adapter_params_t)) return LASER_E_STRUCT;
   if (T < 0 || H < 1 || N < 1 || p->adapters < 0 || p->requests < 0) return LASER_E_RANGE;
-  if (T > (1 << 27) || H > (1 << 28) || N > (1 << 28)) return LASER_E_RANGE;
+  if (T > (1 << 27) || H > (1 << 28) || N > (1 << 28) || p->requests > (1 << 28)) return LASER_E_RANGE;
   if (p->dtype != LASER_DTYPE_F32 && p->dtype != LASER_DTYPE_BF16) return LASER_E_RANGE;
   if (p->out_dtype != LASER_DTYPE_F32 && p->out_dtype != p->dtype) return LASER_E_RANGE;
   if (p->rank < 1) return LASER_E_RANGE;

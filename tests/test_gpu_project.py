@@ -201,3 +201,26 @@ def test_replayed_from_a_graph_and_on_another_stream():
     step(side)
     side.synchronize()
     assert torch.equal(buf.out, want[1])
+
+
+def test_memory_of_a_call_on_another_stream():
+    """A call that allocates for itself, behind other work of its stream: what it works in is not handed
+    out again before it has run."""
+    i = _inputs(70, 512, 64, 16, 8, [1] * 70, BF16, seed=11)
+    dev = {n: (v if torch.is_tensor(v) else torch.from_numpy(v)).cuda() for n, v in i.items()}
+
+    def step(stream=None):
+        return B.project_adapted(dev["x"], dev["w"], dev["a_down"], dev["a_up"], dev["scales"], dev["cuts"],
+                                 dev["which"], out_dtype=torch.float32, stream=stream)
+
+    want = step()
+    side, big = torch.cuda.Stream(), torch.zeros(1 << 28, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(4):
+            big.add_(1.0)
+    got = step(side)
+    size = B.laser_project_workspace_bytes(70, 512, 64, B.make_adapter_params(16, 8, 70, out_dtype=F32))
+    other = [torch.full((size,), 255, dtype=torch.uint8, device="cuda") for _ in range(4)]
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and all(bool((t == 255).all()) for t in other)

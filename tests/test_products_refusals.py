@@ -87,6 +87,7 @@ def test_project():
     bad.struct_bytes = 8
     assert project(bad) == -6
     assert project(T=0) == 0
+    assert project(B.make_adapter_params(8, 2, (1 << 28) + 1)) == -2
     assert B.laser_project_workspace_bytes(8, 60, 5, B.make_adapter_params(8, 2, 3)) == 0
 
 
