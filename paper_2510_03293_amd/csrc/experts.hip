@@ -44,7 +44,7 @@ struct ExpertTiles {
     } else {
       // (offsets are the caller's: whatever they hold, positions stay inside the tables)
       lo = lane < a.E ? min(max(a.offsets[lane], 0), a.slots) : 0;
-      cnt = lane < a.E ? max(min(a.offsets[lane + 1], a.slots) - lo, 0) : 0;
+      cnt = lane < a.E ? max(min(max(a.offsets[lane + 1], 0), a.slots) - lo, 0) : 0;
       if (a.slots > 1 << 24) {
         // (... and sums of what they may hold do not pass 32 bits: no position twice)
         int end = lo + cnt;
