@@ -33,6 +33,18 @@ struct ExpertArgs {
   int H;       // experts_down: columns of out
 };
 
+// The sum over the lanes up to this one.  (Lane exchanges inside the registers: through LDS it takes a microsecond
+// per call where both sizes of tiles are counted.)
+__device__ __forceinline__ int sum_up_to(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // from 1, 2, 4, 8 lanes before, in rows of 16,
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // the last lane of rows 0 and 2 to rows 1 and 3,
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // lane 31 to rows 2 and 3
+  return x;
+}
+
 // The call's experts, one per lane: where their positions begin, how many there are, and, for tiles of
 // BM rows, how many tiles the experts before have.
 struct ExpertTiles {
@@ -58,14 +70,9 @@ struct ExpertTiles {
       }
     }
   }
-  __device__ void count(int lane, int BM) {
+  __device__ void count(int BM) {
     const int tiles = (int)(((unsigned)cnt + BM - 1) / BM);
-    int sum = tiles;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int up = __shfl_up(sum, d);
-      sum += lane >= d ? up : 0;
-    }
+    const int sum = sum_up_to(tiles);
     before = sum - tiles;
     total = __builtin_amdgcn_readlane(sum, 63);
   }
@@ -101,7 +108,7 @@ __device__ __forceinline__ void experts_tiles(const ExpertArgs& a, unsigned char
   // behind the ring: per row of the tile its token (UP) or its slot and weight
   int* const row_of = reinterpret_cast<int*>(ring + TL::kLdsBytes);
   float* const weight_of = reinterpret_cast<float*>(row_of + 2 * BM);
-  tiles.count(lane, BM);
+  tiles.count(BM);
   constexpr int kCols = UP ? BN / 2 : BN;  // output columns of a tile
   constexpr int kWaveCols = kCols / TL::WN;
   const int cols = UP ? a.F : a.H;
@@ -273,8 +280,8 @@ struct Medium {
   static constexpr int kPerCu = 2, kStep = 19, kTile = 120, kOnce = 0;
 };
 template <class HOW, bool UP>
-__device__ __forceinline__ long long cost_of(const ExpertArgs& a, ExpertTiles& tiles, int lane, unsigned units) {
-  tiles.count(lane, HOW::TL::BM);
+__device__ __forceinline__ long long cost_of(const ExpertArgs& a, ExpertTiles& tiles, unsigned units) {
+  tiles.count(HOW::TL::BM);
   constexpr int kCols = UP ? HOW::TL::BN / 2 : HOW::TL::BN;
   const long long all = (long long)tiles.total * (((UP ? a.F : a.H) + kCols - 1) / kCols);
   // (a division in 64 bits would take longer than the rest)
@@ -292,7 +299,7 @@ __global__ __launch_bounds__(TL::kThreads) void experts_kernel(ExpertArgs a, uns
   ExpertTiles tiles;
   tiles.init(a, lane);
   if constexpr (WHEN != kSure) {
-    const bool wide = cost_of<Wide, UP>(a, tiles, lane, units) <= cost_of<Medium, UP>(a, tiles, lane, units);
+    const bool wide = cost_of<Wide, UP>(a, tiles, units) <= cost_of<Medium, UP>(a, tiles, units);
     if (wide != (WHEN == kIfWide)) return;
   }
   experts_tiles<F32, UP, TL>(a, ring, tiles, lane, wave);
