@@ -91,6 +91,8 @@ struct ExpertTiles {
   }
 };
 
+constexpr int kBesideBytes = 2048;  // of a wavefront: 16 rows of 64 results in 16 bits
+
 template <bool F32>
 __device__ __forceinline__ float silu(float g) {
   // g / (1 + exp(-g)); a large negative g divides by infinity and gives -0
@@ -159,7 +161,13 @@ __device__ __forceinline__ void experts_tiles(const ExpertArgs& a, unsigned char
     }
   };
 
+  // With two slots the results are staged beside the ring, so that both slots are filled meanwhile, and
+  // the stores of a tile without gaps (kStores of a wavefront's results and, below, of factors) are still on
+  // their way while the next tile's first steps are multiplied.
+  constexpr bool kBeside = TL::ST == 2;
+  constexpr int kStores = kBeside ? MB * (UP ? NB / 2 : NB) / 2 + (UP ? 0 : MB) : 0;
   int v = blockIdx.x, buf = 0;
+  bool after = false;
   if (v >= total) return;
   find(v);
   int slot = put_row(slot_of(), buf);
@@ -180,7 +188,8 @@ __device__ __forceinline__ void experts_tiles(const ExpertArgs& a, unsigned char
     for (int n = 0; n < NB; ++n)
 #pragma unroll
       for (int m = 0; m < MB; ++m) acc[n][m] = mma_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    tile.run(from, TL::blocks_of(wave, now_rows), acc);
+    tile.template run<kStores>(from, TL::blocks_of(wave, now_rows), acc, after);
+    after = now_rows == BM && now_c0 + kCols <= cols;
 
     if (!UP && threadIdx.x < BM) weight_of[threadIdx.x] = weight;
     if (v < total) slot = put_row(slot, buf ^ 1);
@@ -191,11 +200,15 @@ __device__ __forceinline__ void experts_tiles(const ExpertArgs& a, unsigned char
     asm volatile("" : "+v"(l));
     if (v < total) {
       begin(buf ^ 1, l);
-      if (TL::ST == 2) tile.start_first(from);
+      if (kBeside) {
+        tile.start(from);
+        asm volatile("" ::: "memory");  // (`after` counts what is issued behind these loads)
+      }
     }
-    const unsigned staging = lds + (TL::ST == 2 ? TL::kStage : 0);
+    constexpr int kRoom = kBeside ? kBesideBytes : TL::kLdsBytes / TL::kWaves;
+    const unsigned staging = kBeside ? lds + TL::kLdsBytes + TL::BM * 12 : lds;
     if constexpr (UP) {
-      store_tile<F32 ? kF32 : kBf16, TL, NB / 2>(
+      store_tile<F32 ? kF32 : kBf16, TL, NB / 2, kRoom>(
           staging, wave, l,
           [&](int n, int m) {
             mma_f32x4 y;
@@ -213,7 +226,7 @@ __device__ __forceinline__ void experts_tiles(const ExpertArgs& a, unsigned char
 #pragma unroll
       for (int m = 0; m < MB; ++m) by[m] = weight_of[TL::block_row(wave, m) + (l & 15)];
       if constexpr (F32) {
-        store_tile<kF32, TL, NB>(
+        store_tile<kF32, TL, NB, kRoom>(
             staging, wave, l, [&](int n, int m) { return acc[n][m] * by[m]; },
             [&](int r, int c) -> void* {
               const int h = now_c0 + wn * kWaveCols + c;
@@ -243,7 +256,7 @@ __device__ __forceinline__ void experts_tiles(const ExpertArgs& a, unsigned char
           if (l < 16 && r < now_rows && block * kShared < a.H)
             a.factors[(size_t)row_of[buf * BM + r] * shared_blocks(a.H) + block] = __builtin_bit_cast(float, (127 - 14 + e) << 23);
         }
-        store_tile<kF16, TL, NB>(
+        store_tile<kF16, TL, NB, kRoom>(
             staging, wave, l, [&](int n, int m) { return acc[n][m] * by[m]; },
             [&](int r, int c) -> void* {
               const int h = now_c0 + wn * kWaveCols + c;
@@ -252,11 +265,10 @@ __device__ __forceinline__ void experts_tiles(const ExpertArgs& a, unsigned char
       }
     }
     if (v >= total) break;
-    lds_barrier();  // (everybody's results have left the ring)
-    if (TL::ST == 2)
-      tile.start_second(from);
-    else
+    if (!kBeside) {
+      lds_barrier();  // (everybody's results have left the ring)
       tile.start(from);
+    }
     buf ^= 1;
   }
 }
@@ -512,7 +524,9 @@ __global__ __launch_bounds__(256) void experts_combine_kernel(const void* z, con
 constexpr int kGridMost = 1 << 20;
 
 template <class TL>
-constexpr int lds_of() { return TL::kLdsBytes + TL::BM * 12; }  // the ring, and the table of the tile's rows
+constexpr int lds_of() {  // the ring, the table of the tile's rows, and with two slots room for results
+  return TL::kLdsBytes + TL::BM * 12 + (TL::ST == 2 ? kBesideBytes * TL::kWaves : 0);
+}
 template <class TL, bool UP>
 static long long grid_of(const ExpertArgs& a) {
   // (every expert with rows has at most one tile that is not full, and every tile a row)

@@ -107,7 +107,6 @@ struct Tile {
   static constexpr int kLoads = (BM + BN) / 8 / kWaves;       // load instructions of a wavefront per step
   static constexpr int kStage = (BM + BN) * kStepBytes;
   static constexpr int kLdsBytes = ST * kStage;
-  static constexpr int kStaging = ST == 2 ? kStage : kLdsBytes;  // what store_tile may use of it
   static_assert(kLoads * 8 * kWaves == BM + BN && kWaves % 2 == 0 && ST >= 2, "whole load instructions per wavefront");
   static_assert((ST - 1) * kLoads < 64, "vmcnt counts to 63");
 
@@ -186,16 +185,13 @@ struct Tile {
       if (s < steps) load_all(from, s == steps - 1, s * kStage);
   }
 
-  // start() in two parts: between them only the first half of the ring is being filled
-  __device__ void start_first(const unsigned char* (&from)[kLoads]) { load_all(from, steps == 1, 0); }
-  __device__ void start_second(const unsigned char* (&from)[kLoads]) {
-    if (steps > 1) load_all(from, steps == 2, kStage);
-  }
-
-  // `blocks`: this wavefront's token blocks that have rows; the others' products are left out
-  __device__ void run(const unsigned char* (&from)[kLoads], int blocks, mma_f32x4 (&acc)[NB][MB]) {
+  // `blocks`: this wavefront's token blocks that have rows; the others' products are left out.  AFTER:
+  // with `after`, so many stores at least have been issued since start(); two slots' waits leave them on
+  // their way.
+  template <int AFTER = 0>
+  __device__ void run(const unsigned char* (&from)[kLoads], int blocks, mma_f32x4 (&acc)[NB][MB], bool after = false) {
     if constexpr (ST == 2)
-      run_interleaved(from, blocks, acc);
+      run_interleaved<AFTER>(from, blocks, acc, after);
     else
       run_ring(from, blocks, acc);
     lds_barrier();
@@ -249,7 +245,9 @@ struct Tile {
   // 8192 x 4096 in bf16 took 462 us instead of 387, with one more memory round trip exposed per
   // step; the matrix instructions alone, on the same operands, take 345: the card lowers its
   // clock under them.  Loads in bursts of two per group: 404; the barrier two groups later: 394.)
-  __device__ void run_interleaved(const unsigned char* (&from)[kLoads], int blocks, mma_f32x4 (&acc)[NB][MB]) {
+  template <int AFTER>
+  __device__ void run_interleaved(const unsigned char* (&from)[kLoads], int blocks, mma_f32x4 (&acc)[NB][MB], bool after) {
+    static_assert(kLoads + AFTER < 64, "vmcnt counts to 63");
     constexpr int kGroups = 2 * MB, kAhead = MB - 1;
     mma_u32x4 w[2][NB], t[MB];
     unsigned slot = 0;
@@ -258,7 +256,14 @@ struct Tile {
 #pragma unroll
       for (int g = 0; g < kGroups; ++g) {
         const int behind = g - (kGroups - kAhead);  // groups since the barrier
-        if (next && behind == 0) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (next && behind == 0) {
+          if (AFTER != 0 && after) {  // (the first step's)
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(AFTER) : "memory");
+            after = false;
+          } else {
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+          }
+        }
         if (behind < 0 || next) {
           const int r = (g + kAhead) % kGroups;
           t[r % MB] = token_block(behind < 0 ? slot : slot ^ kStage, r / MB, r % MB);
@@ -283,10 +288,12 @@ struct Tile {
       slot ^= kStage;
     };
     static_assert((kStage & (kStage - 1)) == 0 && NB <= MB, "slots that differ in one bit; weights of half a step read within it");
-    if (steps > 1)
-      asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kLoads) : "memory");
-    else
+    if (steps == 1)
       asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+    else if (AFTER != 0 && after)
+      asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kLoads + AFTER) : "memory");
+    else
+      asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kLoads) : "memory");
 #pragma unroll
     for (int n = 0; n < NB; ++n) w[0][n] = weight_block(0, 0, n);
 #pragma unroll
@@ -300,16 +307,16 @@ struct Tile {
 };
 
 // Results -> memory by whole lines: a wavefront puts the blocks of its part of the tile into a
-// piece of LDS of its own (`lds`: the first of them; the second slot of two, or the whole ring), as
+// piece of LDS of its own (`lds`: the first of them, BYTES each; the whole ring, or room beside it), as
 // many token blocks at a time as fit, and reads them back row by row.  value(n, m): the four
 // outputs of column block n < NC that this lane holds; place(row, column): where the 16 bytes
 // beginning at that row and (wavefront's) column go, or NULL.  (Stores straight from the accumulators reach 16 rows with 32 or 64 bytes each:
 // 98304 x 2048 x 1408 in bf16 took 525 us so and 485 this way, with fp32 results 560 and 515,
 // with none 412.  They go past the caches: nobody reads them soon.)
 enum Stored { kF32, kBf16, kF16 };
-template <Stored AS, class TL, int NC, typename VALUE, typename PLACE>
+template <Stored AS, class TL, int NC, int BYTES = TL::kLdsBytes / TL::kWaves, typename VALUE, typename PLACE>
 __device__ __forceinline__ void store_tile(unsigned lds, int wave, int lane, VALUE value, PLACE place) {
-  constexpr int kBytes = TL::kStaging / TL::kWaves;
+  constexpr int kBytes = BYTES;
   constexpr int kRow = NC * 16 * (AS == kF32 ? 4 : 2);      // bytes of a row
   constexpr int kFit = kBytes / (16 * kRow);
   constexpr int kPass = kFit < TL::MB ? kFit : TL::MB;      // token blocks at a time
@@ -337,7 +344,7 @@ __device__ __forceinline__ void store_tile(unsigned lds, int wave, int lane, VAL
           *(lds_u32x2)(size_t)(row + ((n * 2 + (quad >> 1)) ^ (tok & kTurn)) * 16 + (quad & 1) * 8) = b;
         }
       }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    asm volatile("" ::: "memory");  // (LDS serves a wavefront in order)
     constexpr int kStores = (kPass * 16 + kRows - 1) / kRows;
     mma_u32x4 d[kStores];
     mma_u32x4* to[kStores];
@@ -352,7 +359,7 @@ __device__ __forceinline__ void store_tile(unsigned lds, int wave, int lane, VAL
 #pragma unroll
     for (int i = 0; i < kStores; ++i)
       if (to[i] != nullptr) __builtin_nontemporal_store(d[i], to[i]);
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    asm volatile("" ::: "memory");
   }
 }
 
