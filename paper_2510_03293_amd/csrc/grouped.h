@@ -236,6 +236,57 @@ struct Tile {
     }
   }
 
+  // A ring of 64 x 128 for eight wavefronts of which four take the first half of every step and four the
+  // second, each with 32 tokens x 64 weight rows: 6 blocks read from LDS for 8 products, where
+  // 16 tokens x 64 rows of a whole step read 10.  Both halves' sums are left in LDS, see half_sums().
+  __device__ void run_halves(const unsigned char* (&from)[kLoads], unsigned lds, int wave, int lane) {
+    static_assert(BM == 64 && BN == 128 && kWaves == 8 && kLdsBytes >= 2 * 32 * 1024, "eight parts of 32 x 64");
+    const int half = wave >> 2, rows = wave >> 1 & 1, columns = wave & 1;
+    const unsigned get = lds + (lane & 15) * kStepBytes + ((((lane >> 4) ^ ((lane & 15) >> 1)) * 16) ^ (half * 64));
+    const unsigned tokens = get + rows * 32 * kStepBytes, weights = get + (BM + columns * 64) * kStepBytes;
+    mma_f32x4 acc[4][2];
+#pragma unroll
+    for (int n = 0; n < 4; ++n)
+#pragma unroll
+      for (int m = 0; m < 2; ++m) acc[n][m] = mma_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    unsigned slot = 0;
+    if (steps >= ST)
+      asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((ST - 1) * kLoads) : "memory");
+    else
+      asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+    for (int step = 0; step < steps; ++step) {
+      mma_u32x4 w[4], t[2];
+#pragma unroll
+      for (int m = 0; m < 2; ++m) t[m] = read_lds(tokens + slot + m * 16 * kStepBytes);
+#pragma unroll
+      for (int n = 0; n < 4; ++n) w[n] = read_lds(weights + slot + n * 16 * kStepBytes);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int n = 0; n < 4; ++n)
+#pragma unroll
+        for (int m = 0; m < 2; ++m) acc[n][m] = multiply<F32>(w[n], t[m], acc[n][m]);
+      if (step + 1 == steps) break;
+      if (step + ST <= steps)
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((ST - 2) * kLoads) : "memory");
+      else
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      if (step + ST < steps) load_all(from, step + ST == steps - 1, slot);
+      slot = slot == (ST - 1) * kStage ? 0 : slot + kStage;
+    }
+    lds_barrier();
+#pragma unroll
+    for (int n = 0; n < 4; ++n)
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+        *(lds_f32x4)(size_t)(lds + (((half * 4 + rows * 2 + m) * 8 + columns * 4 + n) * 64 + lane) * 16) = acc[n][m];
+    lds_barrier();
+  }
+  // block `n` of weight rows and `m` of tokens, after run_halves()
+  static __device__ mma_f32x4 half_sums(unsigned lds, int m, int n, int lane) {
+    const unsigned at = lds + ((m * 8 + n) * 64 + lane) * 16;
+    return *(lds_f32x4)(size_t)at + *(lds_f32x4)(size_t)(at + 32 * 1024);
+  }
+
   // Two slots, and a fixed order of everything within a step: 2 MB groups of NB products that
   // share a token block, each with one read from LDS for the group kAhead later and, behind the
   // barrier, one load of the step after the next.  The barrier lies where the last read of the

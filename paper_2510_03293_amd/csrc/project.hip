@@ -510,12 +510,14 @@ __global__ __launch_bounds__(TL::kThreads) void project_kernel(ProjectArgs a) {
 
 // Up to 64 columns (a gate) and adapters of rank up to 64: one launch that reads x once.  The
 // weight rows of a tile are W's and behind them 64 rows of inner matrices, of the first adapters
-// that its 64 rows have; each wavefront has 16 rows, all columns and their v, whose accumulator
-// layout (row 4 (lane / 16) + i) serves as the operand of the second product as it is: which
+// that its 64 rows have.  For the second product each of four wavefronts has 16 rows, all columns and their v,
+// whose accumulator layout (row 4 (lane / 16) + i) serves as the operand as it is: which
 // slot of a matrix instruction is which r is free, as long as U's rows are read the same way.
 // A tile with more adapters makes another pass over its rows for every 128 rows of them.
-// (16384 rows, H = 2048, 64 columns, rank 16: 25 us against 50 with a launch of its own for v, which
-// reads x a second time; bound by reading x, 13 us at the rate of a large copy.)
+// (16384 rows, H = 2048, 64 columns, rank 16: 22 us against 50 with a launch of its own for v, which
+// reads x a second time; reading x alone takes 13 us at the rate of a large copy.  What bounds it is the time of
+// a step, half a microsecond: 24 KiB to LDS, 48 KiB read there, a barrier.  With 80 KiB read, 16 rows and whole
+// steps per wavefront, 23.)
 constexpr int kNarrowColumns = 64, kNarrowRank = 64;
 template <bool F32, bool OUT32, int RB>  // RB: blocks of 16 that hold an adapter's rows
 __global__ __launch_bounds__(512) void project_narrow_kernel(ProjectArgs a) {
@@ -523,7 +525,6 @@ __global__ __launch_bounds__(512) void project_narrow_kernel(ProjectArgs a) {
   constexpr int kRoom = 4 / RB;  // adapters beside W, twice that without
   extern __shared__ __align__(1024) unsigned char ring[];
   int* const ids = reinterpret_cast<int*>(ring + TL::kLdsBytes);
-  mma_f32x4* const found = reinterpret_cast<mma_f32x4*>(ring);  // v between the passes' products: [4 x 16 rows][8 blocks][lane]
   const unsigned lds = (unsigned)(size_t)(lds_bytes)ring;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   TL tile(a.K, lds, wave, lane);
@@ -569,23 +570,16 @@ __global__ __launch_bounds__(512) void project_narrow_kernel(ProjectArgs a) {
           from[i] = (ad < 0 ? a.w : a.a_down + ((size_t)ad * a.R + min(x % (16 * RB), a.R - 1)) * a.K) + piece;
         }
       }
-      mma_f32x4 acc[4][1];
-#pragma unroll
-      for (int n = 0; n < 4; ++n) acc[n][0] = mma_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
       tile.start(from);
-      tile.run(from, 1, acc);
-      // v to the wavefronts that have the columns
-      if (!first || wn == 1)
-#pragma unroll
-        for (int n = 0; n < 4; ++n) found[(wm * 8 + (first ? 0 : wn * 4) + n) * 64 + lane] = acc[n][0];
-      lds_barrier();
+      tile.run_halves(from, lds, wave, lane);
       if (wn == 1) {
         lds_barrier();
         continue;
       }
       if (first)
 #pragma unroll
-        for (int n = 0; n < 4; ++n) y[n][0] = acc[n][0];
+        for (int n = 0; n < 4; ++n) y[n][0] = TL::half_sums(lds, wm, n, lane);
+      const int inner_at = first ? 4 : 0;  // block of the pass's first inner rows
 #pragma unroll
       for (int q = 0; q < 2 * kRoom; ++q) {
         if (held[q] < 0 || __ballot(m == held[q]) == 0) continue;
@@ -599,7 +593,7 @@ __global__ __launch_bounds__(512) void project_narrow_kernel(ProjectArgs a) {
           mma_f32x4 inner[2];  // blocks b and, bf16, b + 1
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            inner[h] = found[(wm * 8 + q * RB + min(b + h, RB - 1)) * 64 + lane];
+            inner[h] = TL::half_sums(lds, wm, inner_at + q * RB + min(b + h, RB - 1), lane);
 #pragma unroll
             for (int i = 0; i < 4; ++i) inner[h][i] = mine && b + h < RB ? inner[h][i] * scale : 0.0f;
           }
@@ -764,26 +758,33 @@ static hipError_t launch_project(ProjectArgs& a, hipStream_t s) {
     const hipError_t err = launch_thin<F32>(a, s);
     return err != hipSuccess ? err : launch_join<F32, OUT32>(a, s);
   }
-  // (a tile of a gate makes its passes one after the other: not where many requests may meet in it)
-  if (a.N <= kNarrowColumns && a.R <= kNarrowRank && (a.requests <= 32 || a.requests <= a.T / 64))
-    return a.R <= 16   ? launch_narrow<F32, OUT32, 1>(a, s)
-           : a.R <= 32 ? launch_narrow<F32, OUT32, 2>(a, s)
-                       : launch_narrow<F32, OUT32, 4>(a, s);
   // (a tile's passes side by side; workgroups without one end at once.  Rank 128, 16384 rows of 40
   // requests: 143 us with one, 126 with four)
   a.lanes = std::max(1, std::min(a.requests, 4));
   const long long rows = (a.T + 63) / 64, tiles = rows * ((a.N + 127) / 128);
+  // A gate in one launch, unless many requests may meet in a tile, which makes its passes one after the other.
+  const bool narrow = a.N <= kNarrowColumns && a.R <= kNarrowRank && (a.requests <= 32 || a.requests <= a.T / 64);
   // Too few tiles for half of the compute units: all in slices, unless the join would have more than
   // kJoinWork products for single threads or there are few steps to cut.  (800 x 247, H = 3624: 67 us in
-  // tiles, 22 in slices; 1078 x 906, H = 640: 24, 27)
+  // tiles, 22 in slices; 1078 x 906, H = 640: 24, 27.)  For a gate's one launch a step takes half a
+  // microsecond, twice that with wide adapters, and the second launch and the sums of slices 10.  (24 requests, 64
+  // columns, one launch and slices: 2000 rows, H = 2048, rank 16 21.6, 17.4, H = 1024 14.3, 15.0; 4000 rows,
+  // H = 2048, rank 16 21.9, 24.3, rank 64 50.6, 28.1)
   constexpr long long kJoinWork = 1 << 25;
-  constexpr int kJoinSteps = 16;
-  if (tiles + rows <= kWorkgroups / 2 && a.K >= kJoinSteps * kStepBytes && (long long)a.T * a.N * a.R <= kJoinWork) {
+  constexpr int kJoinSteps = 16, kLaunchSteps = 18;
+  const int steps = (a.K + kStepBytes - 1) / kStepBytes;
+  if (tiles + rows <= kWorkgroups / 2 && steps >= kJoinSteps && (long long)a.T * a.N * a.R <= kJoinWork) {
     a.slices = slices_for(tiles + rows, a.K);
-    a.in_parts = true;
-    const hipError_t err = launch_inner<F32>(a, a.N, s);
-    return err != hipSuccess ? err : launch_join<F32, OUT32>(a, s);
+    if (!narrow || (long long)steps * (a.R > 16 ? 2 : 1) * (a.slices - 1) > kLaunchSteps * a.slices) {
+      a.in_parts = true;
+      const hipError_t err = launch_inner<F32>(a, a.N, s);
+      return err != hipSuccess ? err : launch_join<F32, OUT32>(a, s);
+    }
   }
+  if (narrow)
+    return a.R <= 16   ? launch_narrow<F32, OUT32, 1>(a, s)
+           : a.R <= 32 ? launch_narrow<F32, OUT32, 2>(a, s)
+                       : launch_narrow<F32, OUT32, 4>(a, s);
   a.slices = slices_for(rows, a.K);
   a.in_parts = a.slices > 1;
   hipError_t err = launch_inner<F32>(a, 0, s);

@@ -58,6 +58,22 @@ def _check(i, out_dtype, dtype, label):
     return out
 
 
+# Gates of up to 64 columns that go in slices, and in one launch with several passes over long rows.
+GATES = [
+    (900, 1288, 64, 16, 5, [1] * 20 + [400, 300, 100]),
+    (1000, 2056, 33, 64, 7, [5] * 12 + [0, 700, 200]),
+    (2100, 1032, 8, 32, 3, [2000, 1]),
+    (4300, 1288, 64, 64, 9, [1] * 20 + [2000, 60, 2100]),
+    (4300, 648, 61, 24, 30, [2] * 40 + [4000]),
+]
+
+
+@pytest.mark.parametrize("dtype,out_dtype", [(BF16, F32), (BF16, BF16), (F32, F32)])
+@pytest.mark.parametrize("shape", GATES, ids=lambda s: "T%d_H%d_N%d_R%d_M%d" % s[:5])
+def test_gates(shape, dtype, out_dtype):
+    _check(_inputs(*shape, dtype, seed=20), out_dtype, dtype, str(shape))
+
+
 @pytest.mark.parametrize("dtype,out_dtype", [(BF16, F32), (BF16, BF16), (F32, F32)])
 @pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "T%d_H%d_N%d_R%d_M%d" % s[:5])
 def test_project(shape, dtype, out_dtype):
