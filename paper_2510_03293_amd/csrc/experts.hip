@@ -15,6 +15,7 @@ namespace laser {
 // a large call's traffic: 16384 tokens, 6 of 64 experts, H = 2048, F = 1408: 811 us with fp32, 730 so.
 // (bf16 would do without factors but be off by 2^-8, which is seen in out.)
 constexpr int kShared = 64;
+constexpr int kMostSlices = 16;  // of the contraction axis, experts_down
 __host__ __device__ inline int shared_blocks(int H) { return (H + kShared - 1) / kShared; }
 
 struct ExpertArgs {
@@ -25,6 +26,7 @@ struct ExpertArgs {
   const float* weights;
   void* out;
   float* factors;  // experts_down, bf16: [slots, shared_blocks(H)]
+  int slices;      // experts_down: parts of the contraction axis; more than one: out is [slices, slots, H] fp32
   int slots;   // T * k
   int k;
   int E;
@@ -103,7 +105,7 @@ __device__ __forceinline__ float silu(float g) {
 // A workgroup computes tiles v, v + grid, ...; what the next one needs first is fetched while
 // the one before is computed: its rows' entries of the permutation before run(), its first
 // steps before the results are written.
-template <bool F32, bool UP, class TL>
+template <bool F32, bool UP, class TL, bool SLICES = false>
 __device__ __forceinline__ void experts_tiles(const ExpertArgs& a, unsigned char* ring, ExpertTiles tiles, int lane, int wave) {
   constexpr int BM = TL::BM, BN = TL::BN, NB = TL::NB, MB = TL::MB;
   static_assert(BM <= TL::kThreads, "one thread per row of the tile");
@@ -118,7 +120,11 @@ __device__ __forceinline__ void experts_tiles(const ExpertArgs& a, unsigned char
   const int total = tiles.total * nt;
   const int wn = wave / TL::WM;
   const unsigned lds = (unsigned)(size_t)(lds_bytes)ring;
-  TL tile(a.K, lds, wave, lane);
+  // (slices of whole steps)
+  const int steps = (a.K + kStepBytes - 1) / kStepBytes, slice = SLICES ? blockIdx.y : 0;
+  const int begin_at = SLICES ? (int)((long long)steps * slice / a.slices) * kStepBytes : 0;
+  const int end_at = SLICES ? min((int)((long long)steps * (slice + 1) / a.slices) * kStepBytes, a.K) : a.K;
+  TL tile(end_at - begin_at, lds, wave, lane);
 
   int e, p0, rows, c0;
   auto find = [&](int v) {
@@ -141,7 +147,7 @@ __device__ __forceinline__ void experts_tiles(const ExpertArgs& a, unsigned char
     // (wide tiles of an expert share its weights through L2 while they are at the same step; narrow
     // ones read them once: 64 experts, 64 tokens 146 -> 130 us with turns, 8 experts, 16 tokens 175 -> 162)
     tile.turn_to(TL::ST == 2 ? e : e * 5 + c0 / kCols);
-    const int piece = TL::piece(wave, lane) * 16 + tile.turn * kStepBytes;
+    const int piece = TL::piece(wave, lane) * 16 + tile.turn * kStepBytes + begin_at;
 #pragma unroll
     for (int i = 0; i < TL::kLoads; ++i) {
       const int r = TL::row(wave, lane, i);
@@ -225,12 +231,13 @@ __device__ __forceinline__ void experts_tiles(const ExpertArgs& a, unsigned char
       float by[MB];
 #pragma unroll
       for (int m = 0; m < MB; ++m) by[m] = weight_of[TL::block_row(wave, m) + (l & 15)];
-      if constexpr (F32) {
+      if constexpr (F32 || SLICES) {
         store_tile<kF32, TL, NB, kRoom>(
             staging, wave, l, [&](int n, int m) { return acc[n][m] * by[m]; },
             [&](int r, int c) -> void* {
               const int h = now_c0 + wn * kWaveCols + c;
-              return r < now_rows && h < a.H ? static_cast<float*>(a.out) + (size_t)row_of[buf * BM + r] * a.H + h : nullptr;
+              const size_t slot = (size_t)slice * a.slots + row_of[buf * BM + r];
+              return r < now_rows && h < a.H ? static_cast<float*>(a.out) + slot * a.H + h : nullptr;
             });
       } else {
         // In 16 bits, see the top of the file: the largest finite value of the row's kShared columns
@@ -315,6 +322,16 @@ __global__ __launch_bounds__(TL::kThreads) void experts_kernel(ExpertArgs a, uns
     if (wide != (WHEN == kIfWide)) return;
   }
   experts_tiles<F32, UP, TL>(a, ring, tiles, lane, wave);
+}
+
+// Sums over slices of the contraction axis.
+template <bool F32, class TL>
+__global__ __launch_bounds__(TL::kThreads) void experts_slices_kernel(ExpertArgs a) {
+  extern __shared__ __align__(1024) unsigned char ring[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  ExpertTiles tiles;
+  tiles.init(a, lane);
+  experts_tiles<F32, false, TL, true>(a, ring, tiles, lane, wave);
 }
 
 // ---- a few tokens -------------------------------------------------------------------
@@ -521,6 +538,33 @@ __global__ __launch_bounds__(256) void experts_combine_kernel(const void* z, con
   }
 }
 
+// The same from sums of slices, [slices, T k, H] fp32: a slot's slices first.  One thread per four columns.
+template <bool F32>
+__global__ __launch_bounds__(256) void experts_join_kernel(const float* parts, int slices, const int32_t* ids, const void* base,
+                                                           void* out, int T, int H, int k, int first, int E) {
+  const int pieces = H / 4;
+  const size_t all = (size_t)T * pieces, next = (size_t)T * k * H;
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (size_t)gridDim.x * 256) {
+    const size_t t = i / pieces;
+    const int h = (int)(i - t * pieces) * 4;
+    mma_f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (base != nullptr) y = load4<F32>(base, t * H + h);
+    for (int j = 0; j < k; ++j) {
+      if (ids != nullptr && (unsigned)(ids[t * k + j] - first) >= (unsigned)E) continue;
+      const float* const row = parts + (t * k + j) * H + h;
+      mma_f32x4 part[kMostSlices];
+#pragma unroll
+      for (int s = 0; s < kMostSlices; ++s)
+        part[s] = s < slices ? *reinterpret_cast<const mma_f32x4*>(row + s * next) : mma_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      mma_f32x4 sum = part[0];
+#pragma unroll
+      for (int s = 1; s < kMostSlices; ++s) sum += part[s];
+      y += sum;
+    }
+    store4<F32>(out, t * H + h, y);
+  }
+}
+
 constexpr int kGridMost = 1 << 20;
 
 template <class TL>
@@ -573,6 +617,33 @@ static hipError_t launch_products(const ExpertArgs& a, hipStream_t s) {
   return launch_experts<F32, UP, LOW, kSure>(a, kGridMost, s);
 }
 
+// experts_down with tiles for at most half of the compute units and a long way along the contraction axis
+// takes that in slices, at least kSliceSteps steps each.  (69 tokens on 5 experts, H = 248, F = 12760: 120 us in one, 18
+// in slices; 16 on 8, H = 512, F = 2416 29, 15; 300 on 4, H = 512, F = 1024 18.5, 15; 700 on one, H = 1024, F = 2048 31, 20)
+constexpr int kSliceSteps = 8, kSliceWorkgroups = 256;
+template <bool F32>
+using SliceTile = Tile<F32, 64, 128, 2, 2, 3>;
+template <bool F32>
+static int slices_of(const ExpertArgs& a) {
+  const long long units = grid_of<SliceTile<F32>, false>(a), steps = (a.K + kStepBytes - 1) / kStepBytes;
+  return (int)std::max<long long>(1, std::min<long long>({kMostSlices, kSliceWorkgroups / units, steps / kSliceSteps}));
+}
+// (values times slices are at most those of kSliceWorkgroups tiles)
+static size_t slices_bytes(size_t slots, int H) {
+  return std::min<size_t>(slots * H * kMostSlices, (size_t)kSliceWorkgroups * 64 * 128) * 4;
+}
+template <bool F32>
+static hipError_t launch_slices(const ExpertArgs& a, hipStream_t s) {
+  using TL = SliceTile<F32>;
+  static LdsAttr attr;
+  const void* fn = reinterpret_cast<const void*>(&experts_slices_kernel<F32, TL>);
+  hipError_t err = allow_dynamic_lds(fn, lds_of<TL>(), attr);
+  if (err != hipSuccess) return err;
+  hipLaunchKernelGGL((experts_slices_kernel<F32, TL>), dim3((unsigned)grid_of<TL, false>(a), a.slices), dim3(TL::kThreads),
+                     lds_of<TL>(), s, a);
+  return hipGetLastError();
+}
+
 static int check_experts(int32_t T, int32_t H, int32_t F, int32_t E, const laser_experts_params_t* p) {
   if (!p) return LASER_E_NULL;
   if (p->struct_bytes != sizeof(laser_experts_params_t)) return LASER_E_STRUCT;
@@ -589,6 +660,9 @@ static int check_experts(int32_t T, int32_t H, int32_t F, int32_t E, const laser
 static bool are_few(int T, int slots, int F) { return T <= kFewTokens && slots <= kFewSlots && F <= 1 << 17; }
 
 static size_t whole_256(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
+static size_t summands_bytes(size_t slots, int H, bool f32) {
+  return f32 ? whole_256(slots * H * 4) : whole_256(slots * H * 2) + whole_256(slots * shared_blocks(H) * 4);
+}
 static bool misaligned(const void* p) { return ((uintptr_t)p & 15) != 0; }
 
 // Without tables: one expert that takes every token once.
@@ -644,8 +718,7 @@ extern "C" size_t laser_experts_workspace_bytes(int32_t T, int32_t H, int32_t F,
                                                 const laser_experts_params_t* params) {
   if (check_experts(T, H, F, E, params) != LASER_OK) return 0;
   const size_t slots = (size_t)T * params->k;
-  return params->dtype == LASER_DTYPE_F32 ? whole_256(slots * H * 4) + 256
-                                          : whole_256(slots * H * 2) + whole_256(slots * shared_blocks(H) * 4) + 256;
+  return summands_bytes(slots, H, params->dtype == LASER_DTYPE_F32) + whole_256(slices_bytes(slots, H)) + 256;
 }
 
 extern "C" int laser_experts_down(const void* act, const void* w_down, int32_t T, int32_t H, int32_t F, int32_t E,
@@ -691,6 +764,18 @@ extern "C" int laser_experts_down(const void* act, const void* w_down, int32_t T
     auto* const kernel = f32 ? (T == 1 ? pick(std::true_type{}, std::true_type{}) : pick(std::true_type{}, std::false_type{}))
                              : (T == 1 ? pick(std::false_type{}, std::true_type{}) : pick(std::false_type{}, std::false_type{}));
     hipLaunchKernelGGL(kernel, grid, block, 0, s, a, expert_ids, params->first_expert, base, out, T);
+    return hipGetLastError() == hipSuccess ? LASER_OK : LASER_E_LAUNCH;
+  }
+  a.slices = f32 ? slices_of<true>(a) : slices_of<false>(a);
+  if (a.slices > 1) {
+    float* const parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + summands_bytes(a.slots, H, f32));
+    a.out = parts;
+    const hipError_t err = f32 ? launch_slices<true>(a, s) : launch_slices<false>(a, s);
+    if (err != hipSuccess) return LASER_E_LAUNCH;
+    const unsigned grid = (unsigned)std::min<size_t>(((size_t)T * (H / 4) + 255) / 256, 1 << 16);
+    auto* const join = f32 ? &experts_join_kernel<true> : &experts_join_kernel<false>;
+    hipLaunchKernelGGL(join, dim3(grid), dim3(256), 0, s, parts, a.slices, expert_ids, base, out, T, H, params->k,
+                       params->first_expert, E);
     return hipGetLastError() == hipSuccess ? LASER_OK : LASER_E_LAUNCH;
   }
   const hipError_t err = f32 ? launch_products<true, false>(a, s) : launch_products<false, false>(a, s);

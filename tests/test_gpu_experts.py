@@ -77,6 +77,20 @@ def test_down(shape, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("shape", [
+    (69, 248, 2760, 5, 1, 5, 0, 0.3),
+    (5, 72, 8200, 2, 2, 2, 0, 0.0),
+    (40, 264, 1544, 6, 3, 24, 12, 0.5),     # a share of the experts
+    (333, 136, 1032, 3, 2, 3, 0, 2.0),      # an expert that takes nearly everything
+    (6, 8, 4096, 64, 16, 64, 0, 0.0),       # steps without a rest
+    (700, 264, 1160, 1, 1, 1, 0, 0.0),
+], ids=lambda s: "T%d_H%d_F%d_E%d_k%d" % s[:5])
+def test_down_in_slices(shape, dtype):
+    """Few rows and a long way along the contraction axis."""
+    test_down(shape, dtype)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 def test_one_expert_for_every_token(dtype):
     """Without tables: a shared expert; its output is the base of the routed ones, in place."""
     rng = np.random.default_rng(7)
