@@ -617,16 +617,19 @@ static hipError_t launch_products(const ExpertArgs& a, hipStream_t s) {
   return launch_experts<F32, UP, LOW, kSure>(a, kGridMost, s);
 }
 
-// experts_down with tiles for at most half of the compute units and a long way along the contraction axis
-// takes that in slices, at least kSliceSteps steps each.  (69 tokens on 5 experts, H = 248, F = 12760: 120 us in one, 18
-// in slices; 16 on 8, H = 512, F = 2416 29, 15; 300 on 4, H = 512, F = 1024 18.5, 15; 700 on one, H = 1024, F = 2048 31, 20)
-constexpr int kSliceSteps = 8, kSliceWorkgroups = 256;
+// experts_down with few tiles and a long way along the contraction axis takes that in slices, at least
+// kSliceSteps steps each, as many as make kSliceWorkgroups of the tiles.  (69 tokens on 5 experts, H = 248, F = 12760:
+// 120 us in one, 18 in slices; 16 on 8, H = 512, F = 2416 29, 15; 300 on 4, H = 512, F = 1024 18.5, 15; 700 on one,
+// H = 1024, F = 2048 31, 20.)  Half of that where an expert's tiles do not share its weights, which then
+// bound the call: 500 on 4, H = 1024, F = 4096 with 256 49 us, with 512 28; 16 on 8, H = 4096, F = 14336 145, 170.
+constexpr int kSliceSteps = 8, kSliceWorkgroups = 512, kSharedRows = 32;
 template <bool F32>
 using SliceTile = Tile<F32, 64, 128, 2, 2, 3>;
 template <bool F32>
 static int slices_of(const ExpertArgs& a) {
   const long long units = grid_of<SliceTile<F32>, false>(a), steps = (a.K + kStepBytes - 1) / kStepBytes;
-  return (int)std::max<long long>(1, std::min<long long>({kMostSlices, kSliceWorkgroups / units, steps / kSliceSteps}));
+  const int workgroups = a.slots >= (long long)kSharedRows * a.E ? kSliceWorkgroups : kSliceWorkgroups / 2;
+  return (int)std::max<long long>(1, std::min<long long>({kMostSlices, workgroups / units, steps / kSliceSteps}));
 }
 // (values times slices are at most those of kSliceWorkgroups tiles)
 static size_t slices_bytes(size_t slots, int H) {

@@ -91,6 +91,16 @@ def test_down_in_slices(shape, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("shape", [
+    (2600, 1032, 1160, 4, 2, 4, 0, 0.1),    # the widest tiles
+    (1500, 1032, 1160, 12, 1, 12, 0, 0.0),  # tiles for which those would be too few
+], ids=lambda s: "T%d_H%d_F%d_E%d_k%d" % s[:5])
+def test_down_in_tiles(shape, dtype):
+    """Rows enough not to go in slices, of many steps."""
+    test_down(shape, dtype)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 def test_one_expert_for_every_token(dtype):
     """Without tables: a shared expert; its output is the base of the routed ones, in place."""
     rng = np.random.default_rng(7)
