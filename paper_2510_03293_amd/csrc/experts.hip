@@ -659,8 +659,14 @@ static int check_experts(int32_t T, int32_t H, int32_t F, int32_t E, const laser
   return LASER_OK;
 }
 
-// (F: a dimension of the grid)
-static bool are_few(int T, int slots, int F) { return T <= kFewTokens && slots <= kFewSlots && F <= 1 << 17; }
+// Whether a call goes as products with single vectors, `rows` rows of an expert's matrices for each slot.  (F: a
+// dimension of the grid.)  Rows that are shorter than a load instruction leave lanes without work, which
+// tiles do not once there are many: 8 slots, up of H = 248, F = 8320 39 us so, 22 in tiles, of H = 400, F = 1408 7.6,
+// 7.7; 18 slots, up of H = 400, F = 1408 15.7, 12.9, down of F = 400, H = 1024 11.6, 15.
+constexpr int kShortBytes = 1024, kShortRows = 1 << 15;
+static bool are_few(int T, const ExpertArgs& a, long long rows) {
+  return T <= kFewTokens && a.slots <= kFewSlots && a.F <= 1 << 17 && (a.K >= kShortBytes || a.slots * rows <= kShortRows);
+}
 
 static size_t whole_256(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
 static size_t summands_bytes(size_t slots, int H, bool f32) {
@@ -705,7 +711,7 @@ extern "C" int laser_experts_up(const void* hidden, const void* w_up, int32_t T,
   a.H = H;
   clear_stale_error();
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  if (are_few(T, a.slots, F)) {
+  if (are_few(T, a, 2ll * F)) {
     const int columns = T == 1 ? 1 : 2;
     const dim3 grid(a.slots, (F + 4 * columns - 1) / (4 * columns));
     auto* const kernel = f32 ? (T == 1 ? &experts_up_few_kernel<true, true, 1> : &experts_up_few_kernel<true, false, 2>)
@@ -755,7 +761,7 @@ extern "C" int laser_experts_down(const void* act, const void* w_down, int32_t T
   a.H = H;
   clear_stale_error();
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  if (are_few(T, a.slots, F)) {
+  if (are_few(T, a, H)) {
     const int rows = H >= 16 * compute_units() ? 8 : H >= 8 * compute_units() ? 4 : 2;
     const dim3 grid((H + rows - 1) / rows), block(64 * kFewWaves);
     auto pick = [&](auto is32, auto once) {

@@ -38,6 +38,8 @@ SHAPES = [
     (900, 1152, 1216, 2, 1, 2, 0, 1.0),    # ... and without
     (1000, 1216, 1152, 4, 4, 32, 8, 0.0),  # a share with fewer rows than the tables hold for as many experts
     (515, 2048, 1280, 1, 1, 1, 0, 0.0),
+    (3, 72, 2504, 21, 8, 24, 2, 0.0),      # few tokens whose rows are short and many
+    (2, 2088, 72, 30, 9, 30, 0, 0.0),
 ]
 
 
