@@ -653,25 +653,25 @@ __global__ __launch_bounds__(512) void project_narrow_kernel(ProjectArgs a) {
 constexpr int kThinRows = 512, kThinValues = 1 << 16;
 static bool is_thin(int T, int N) { return T <= kThinRows && (long long)T * N <= kThinValues; }
 // slices so that `units` tiles become about as many workgroups as there are compute units
-constexpr int kWorkgroups = 256;
-static int slices_for(long long units, int K) {
+constexpr int kWorkgroups = 256, kSliceWorkgroups = 512;
+static int slices_for(long long units, int K, int workgroups) {
   const int steps = (K + kStepBytes - 1) / kStepBytes;
-  return (int)std::max<long long>(1, std::min<long long>({kMostSlices, kWorkgroups / units, steps}));
+  return (int)std::max<long long>(1, std::min<long long>({kMostSlices, workgroups / units, steps}));
 }
 
 static size_t whole(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
 struct ProjectLayout {
   size_t adapter, inner, parts, shared, total;
 };
-// (each part grows with T.  Rows times slices, and values of out times slices, are at most those of kWorkgroups
+// (each part grows with T.  Rows times slices, and values of out times slices, are at most those of kSliceWorkgroups
 // tiles of 64 rows and of 64 x 128)
 static ProjectLayout project_layout(int T, int N, const laser_adapter_params_t* p) {
   ProjectLayout L;
   L.adapter = 0;
   L.inner = whole((size_t)T * 4);
   L.parts = L.inner + whole((size_t)T * p->rank * (p->dtype == LASER_DTYPE_F32 ? 4 : 6));
-  L.shared = L.parts + whole(std::min<size_t>((size_t)T * kMostSlices, kWorkgroups * 64) * p->rank * 4);
-  L.total = L.shared + whole(std::min<size_t>((size_t)T * N * kMostSlices, kWorkgroups * 64 * 128) * 4) + 256;
+  L.shared = L.parts + whole(std::min<size_t>((size_t)T * kMostSlices, kSliceWorkgroups * 64) * p->rank * 4);
+  L.total = L.shared + whole(std::min<size_t>((size_t)T * N * kMostSlices, kSliceWorkgroups * 64 * 128) * 4) + 256;
   return L;
 }
 
@@ -764,17 +764,17 @@ static hipError_t launch_project(ProjectArgs& a, hipStream_t s) {
   const long long rows = (a.T + 63) / 64, tiles = rows * ((a.N + 127) / 128);
   // A gate in one launch, unless many requests may meet in a tile, which makes its passes one after the other.
   const bool narrow = a.N <= kNarrowColumns && a.R <= kNarrowRank && (a.requests <= 32 || a.requests <= a.T / 64);
-  // Too few tiles for half of the compute units: all in slices, unless the join would have more than
-  // kJoinWork products for single threads or there are few steps to cut.  (800 x 247, H = 3624: 67 us in
-  // tiles, 22 in slices; 1078 x 906, H = 640: 24, 27.)  For a gate's one launch a step takes half a
-  // microsecond, twice that with wide adapters, and the second launch and the sums of slices 10.  (24 requests, 64
-  // columns, one launch and slices: 2000 rows, H = 2048, rank 16 21.6, 17.4, H = 1024 14.3, 15.0; 4000 rows,
-  // H = 2048, rank 16 21.9, 24.3, rank 64 50.6, 28.1)
+  // Too few tiles for all compute units: all in slices, for one workgroup per compute unit or two, unless the
+  // join would have more than kJoinWork products for single threads or there are few steps to cut.  (800 x 247,
+  // H = 3624: 67 us in tiles, 22 in slices; 3000 x 256, H = 2048: 44, 33; 1078 x 906, H = 640: 24, 27.)  For a
+  // gate's one launch a step takes half a microsecond, twice that with wide adapters, and the second launch and the
+  // sums of slices 10.  (24 requests, 64 columns, one launch and slices: 2000 rows, H = 2048, rank 16 21.6, 17.4,
+  // H = 1024 14.3, 15.0; 4000 rows, H = 2048, rank 16 21.9, 24.3, rank 64 50.6, 28.1)
   constexpr long long kJoinWork = 1 << 25;
   constexpr int kJoinSteps = 16, kLaunchSteps = 18;
   const int steps = (a.K + kStepBytes - 1) / kStepBytes;
-  if (tiles + rows <= kWorkgroups / 2 && steps >= kJoinSteps && (long long)a.T * a.N * a.R <= kJoinWork) {
-    a.slices = slices_for(tiles + rows, a.K);
+  if (tiles + rows <= kSliceWorkgroups / 2 && steps >= kJoinSteps && (long long)a.T * a.N * a.R <= kJoinWork) {
+    a.slices = slices_for(tiles + rows, a.K, tiles + rows <= kWorkgroups / 2 ? kWorkgroups : kSliceWorkgroups);
     if (!narrow || (long long)steps * (a.R > 16 ? 2 : 1) * (a.slices - 1) > kLaunchSteps * a.slices) {
       a.in_parts = true;
       const hipError_t err = launch_inner<F32>(a, a.N, s);
@@ -785,7 +785,7 @@ static hipError_t launch_project(ProjectArgs& a, hipStream_t s) {
     return a.R <= 16   ? launch_narrow<F32, OUT32, 1>(a, s)
            : a.R <= 32 ? launch_narrow<F32, OUT32, 2>(a, s)
                        : launch_narrow<F32, OUT32, 4>(a, s);
-  a.slices = slices_for(rows, a.K);
+  a.slices = slices_for(rows, a.K, kWorkgroups);
   a.in_parts = a.slices > 1;
   hipError_t err = launch_inner<F32>(a, 0, s);
   if (err != hipSuccess) return err;
