@@ -287,9 +287,9 @@ __device__ __forceinline__ void experts_tiles(const ExpertArgs& a, unsigned char
 // What the two would take, in twentieths of a microsecond: as many rounds of tiles as workgroups run
 // side by side, of so much per step and so much before and behind the steps (fitted to the figures
 // below; of a compute unit's two workgroups with 128 x 128 each has half of the steps' rate).
-//   us with 128 x 128, 256 x 256:  up of H = 2048, F = 1408, 64 experts, 2048 tokens 248, 230, 4096 tokens 390, 327;
-//   down of the same 162, 166 and 274, 240;  16 of the 64 experts, 1501 tokens, 2600 rows 27, 42;  up of H = 4096,
-//   F = 2048, 8 experts, 1024 tokens 141, 109;  down of F = 4096, H = 4096, 8 experts, 1500 tokens 147, 164
+//   us with 128 x 128, 256 x 256:  up of H = 2048, F = 1408, 64 experts, 2048 tokens 226, 204, 4096 tokens 354,
+//   303;  down of the same 143, 149 and 234, 212;  16 of the 64 experts, down of 1910 rows 38, 51, of 3763 rows 57,
+//   54;  8 experts, H = 4096, up of F = 2048 and 1024 tokens 114, 92, down of F = 4096 and 1500 tokens 140, 187
 struct Wide {
   using TL = Tile<false, 256, 256, 2, 4, 2>;
   static constexpr int kPerCu = 1, kStep = 25, kTile = 120, kOnce = 120;
@@ -431,9 +431,9 @@ __global__ __launch_bounds__(256) void experts_up_few_kernel(ExpertArgs a) {
 }
 
 // ROWS rows of the matrices (columns of out) per workgroup, as many as leave two workgroups for every
-// compute unit (H = 2048, one token: eight rows 11.7 us, four 11.1; H = 128, three tokens: eight 26.8, two 19.4).  Its wavefronts take the slots
-// in turn, and where there are fewer slots than wavefronts, parts of the rows as well; what they
-// find waits in LDS for its place in the sums, which run in slot order.
+// compute unit (H = 2048, one token: eight rows 11.7 us, four 11.1; H = 128, three tokens: eight 26.8,
+// two 19.4).  Its wavefronts take the slots in turn, and where there are fewer slots than wavefronts,
+// parts of the rows as well; what they find waits in LDS for its place in the sums, which run in slot order.
 constexpr int kFewWaves = 8;
 template <bool F32, bool ONCE, int ROWS>
 __global__ __launch_bounds__(64 * kFewWaves) void experts_down_few_kernel(ExpertArgs a, const int32_t* ids, int first,

@@ -254,10 +254,11 @@ __global__ __launch_bounds__(256) void adapter_join_kernel(ProjectArgs a) {
 }
 
 // Many rows: tiles of 64 rows against 128 rows of inner matrices at a time, the first adapters that
-// the 64 rows have, then the next, through LDS (blockIdx.z: every lanes-th of those passes).  blockIdx.y: slice of the contraction axis
-// where there are not tiles enough for all compute units; then sums of slices, joined below.
+// the 64 rows have, then the next, through LDS (blockIdx.z: every lanes-th of those passes; behind them
+// the shared projection's columns).  blockIdx.y: slice of the contraction axis where there are not
+// tiles enough for all compute units; then sums of slices, joined below.
 // (4096 rows, H = 4096, rank 64: 16 rows per workgroup, as thin calls do, read the matrices four times
-// as often and not by whole lines; 41 us, 26 this way.)
+// as often and not by whole lines; 41 us, 22 this way.)
 template <bool F32, int RB>
 __global__ __launch_bounds__(512) void adapter_tiles_kernel(ProjectArgs a) {
   using TL = Tile<F32, 64, 128, 4, 2, 3>;
