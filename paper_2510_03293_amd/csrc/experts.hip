@@ -592,14 +592,16 @@ static hipError_t launch_experts(const ExpertArgs& a, long long most, hipStream_
 }
 
 // Which tiles.  bf16, by the rows per expert if they were even, of which the host knows an upper bound
-// (the call's experts may be a share of the layer's): few, 64 x 128 (48 rows per expert of H = 2048, F = 1408: up
-// 167 us, with 128 x 128 182; 192 rows: 304, 248); more, what cost_of says, unless the rows have so few
-// steps that 256 x 256 cannot win (8000 tokens, 2000 rows per expert, 128 x 128 and 256 x 256: down of F = 320 70,
-// 76, F = 1024 109, 116; up of H = 136 62, 80, H = 640 103, 102, H = 1024 145, 141).
+// (the call's experts may be a share of the layer's): few, 64 x 128, whose weights go past the caches and are read
+// again where an expert has more than 64 rows; more, what cost_of says.  (64 x 128 and 128 x 128, up of H = 2048,
+// F = 1408, 64 experts, popularity even: 48 rows per expert 128, 142 us, 58 rows 153, 141, 66 rows 195, 145, 94 rows
+// 231, 152; skewed: 52 rows 152, 154, 58 rows 163, 154.  Down of the same, even: 48 rows 80, 88, 58 rows 93, 89,
+// 94 rows 137, 97.)  Where the rows have so few steps that 256 x 256 cannot win, 128 x 128 (8000 tokens, 2000 rows per expert, 128 x 128 and 256 x 256: down of
+// F = 320 70, 76, F = 1024 109, 116; up of H = 136 62, 80, H = 640 103, 102, H = 1024 145, 141).
 // fp32 is bound by its matrix instructions (a sixteenth of the rate) as soon as there are tiles for
 // all compute units; before that, small tiles are more of them (333 tokens, 33 experts, 516 x 212: 30 us
 // with tiles of 64 x 128, 20 with 32 x 64; 4000 tokens, 8 experts, 1024 x 1024: 333 and 391).
-constexpr int kSomeRows = 96, kWideSteps = 18;
+constexpr int kSomeRows = 56, kWideSteps = 18;
 template <bool F32, bool UP>
 static hipError_t launch_products(const ExpertArgs& a, hipStream_t s) {
   // (most experts then have one tile of rows, so their weights are read once: 64 tokens on 64 experts 128 us,
