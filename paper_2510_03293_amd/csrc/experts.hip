@@ -7,16 +7,11 @@
 
 namespace laser {
 
-// What experts_down keeps of a slot until its token's sum is taken.  fp32 calls: the weighted product
-// in fp32.  bf16 calls: in fp16, 11 significant bits, a power of two as factor for every kShared
-// columns; a summand is then off by 2^-11 of itself (and 2^-39 of the largest of its kShared), while
-// out is rounded by 2^-8 of the sum, so that what a call is off by does not change in two
-// digits.  The sum itself is taken in fp32.  Written and read once each, these values are the largest part of
-// a large call's traffic: 16384 tokens, 6 of 64 experts, H = 2048, F = 1408: 811 us with fp32, 730 so.
-// (bf16 would do without factors but be off by 2^-8, which is seen in out.)
-constexpr int kShared = 64;
+// What experts_down keeps of a slot until its token's sum is taken: the weighted product in fp32, whatever the
+// type of the call.  Experts of a token may cancel, so that no rounding of a summand is small beside out's own.
+// Written and read once each, these values are the largest part of a large call's traffic: 16384 tokens,
+// 6 of 64 experts, H = 2048: 805 MB each way.
 constexpr int kMostSlices = 16;  // of the contraction axis, experts_down
-__host__ __device__ inline int shared_blocks(int H) { return (H + kShared - 1) / kShared; }
 
 struct ExpertArgs {
   const unsigned char* x;    // rows of the token operand
@@ -25,8 +20,7 @@ struct ExpertArgs {
   const int32_t* offsets;      // [E + 1] of the call's experts
   const float* weights;
   void* out;
-  float* factors;  // experts_down, bf16: [slots, shared_blocks(H)]
-  int slices;      // experts_down: parts of the contraction axis; more than one: out is [slices, slots, H] fp32
+  int slices;      // experts_down: parts of the contraction axis; out is [slices, slots, H] fp32
   int slots;   // T * k
   int k;
   int E;
@@ -93,7 +87,7 @@ struct ExpertTiles {
   }
 };
 
-constexpr int kBesideBytes = 2048;  // of a wavefront: 16 rows of 64 results in 16 bits
+constexpr int kBesideBytes = 2048;  // of a wavefront: 16 rows of 128 bytes of results
 
 template <bool F32>
 __device__ __forceinline__ float silu(float g) {
@@ -168,10 +162,10 @@ __device__ __forceinline__ void experts_tiles(const ExpertArgs& a, unsigned char
   };
 
   // With two slots the results are staged beside the ring, so that both slots are filled meanwhile, and
-  // the stores of a tile without gaps (kStores of a wavefront's results and, below, of factors) are still on
-  // their way while the next tile's first steps are multiplied.
+  // the stores of a tile without gaps (kStores of a wavefront, 1 KiB each) are still on their way while the
+  // next tile's first steps are multiplied.
   constexpr bool kBeside = TL::ST == 2;
-  constexpr int kStores = kBeside ? MB * (UP ? NB / 2 : NB) / 2 + (UP ? 0 : MB) : 0;
+  constexpr int kStores = !kBeside ? 0 : UP ? MB * (NB / 2) / 2 : MB * NB;
   int v = blockIdx.x, buf = 0;
   bool after = false;
   if (v >= total) return;
@@ -214,7 +208,7 @@ __device__ __forceinline__ void experts_tiles(const ExpertArgs& a, unsigned char
     constexpr int kRoom = kBeside ? kBesideBytes : TL::kLdsBytes / TL::kWaves;
     const unsigned staging = kBeside ? lds + TL::kLdsBytes + TL::BM * 12 : lds;
     if constexpr (UP) {
-      store_tile<F32 ? kF32 : kBf16, TL, NB / 2, kRoom>(
+      store_tile<F32, TL, NB / 2, kRoom>(
           staging, wave, l,
           [&](int n, int m) {
             mma_f32x4 y;
@@ -231,45 +225,17 @@ __device__ __forceinline__ void experts_tiles(const ExpertArgs& a, unsigned char
       float by[MB];
 #pragma unroll
       for (int m = 0; m < MB; ++m) by[m] = weight_of[TL::block_row(wave, m) + (l & 15)];
-      if constexpr (F32 || SLICES) {
-        store_tile<kF32, TL, NB, kRoom>(
-            staging, wave, l, [&](int n, int m) { return acc[n][m] * by[m]; },
+      // (beside the ring there is room for half of a wavefront's columns at a time)
+      constexpr int kAtOnce = kBeside ? NB / 2 : NB;
+#pragma unroll
+      for (int n0 = 0; n0 < NB; n0 += kAtOnce)
+        store_tile<true, TL, kAtOnce, kRoom>(
+            staging, wave, l, [&](int n, int m) { return acc[n0 + n][m] * by[m]; },
             [&](int r, int c) -> void* {
-              const int h = now_c0 + wn * kWaveCols + c;
+              const int h = now_c0 + wn * kWaveCols + n0 * 16 + c;
               const size_t slot = (size_t)slice * a.slots + row_of[buf * BM + r];
               return r < now_rows && h < a.H ? static_cast<float*>(a.out) + slot * a.H + h : nullptr;
             });
-      } else {
-        // In 16 bits, see the top of the file: the largest finite value of the row's kShared columns
-        // decides the factor 2^(14 - e) that brings it into [2^14, 2^15).
-        static_assert(kWaveCols == kShared, "a wavefront's columns share a factor");
-        const int block = (now_c0 + wn * kWaveCols) / kShared;
-#pragma unroll
-        for (int m = 0; m < MB; ++m) {
-          float most = 0.0f;
-#pragma unroll
-          for (int n = 0; n < NB; ++n)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              acc[n][m][i] *= by[m];
-              const float size = fabsf(acc[n][m][i]);
-              most = size < __builtin_inff() ? fmaxf(most, size) : most;
-            }
-          most = fmaxf(most, __shfl_xor(most, 16));
-          most = fmaxf(most, __shfl_xor(most, 32));
-          const int e = max((int)(__builtin_bit_cast(unsigned, most) >> 23) - 127, -100);
-          by[m] = __builtin_bit_cast(float, (127 + 14 - e) << 23);
-          const int r = TL::block_row(wave, m) + (l & 15);
-          if (l < 16 && r < now_rows && block * kShared < a.H)
-            a.factors[(size_t)row_of[buf * BM + r] * shared_blocks(a.H) + block] = __builtin_bit_cast(float, (127 - 14 + e) << 23);
-        }
-        store_tile<kF16, TL, NB, kRoom>(
-            staging, wave, l, [&](int n, int m) { return acc[n][m] * by[m]; },
-            [&](int r, int c) -> void* {
-              const int h = now_c0 + wn * kWaveCols + c;
-              return r < now_rows && h < a.H ? static_cast<unsigned short*>(a.out) + (size_t)row_of[buf * BM + r] * a.H + h : nullptr;
-            });
-      }
     }
     if (v >= total) break;
     if (!kBeside) {
@@ -485,56 +451,32 @@ __global__ __launch_bounds__(64 * kFewWaves) void experts_down_few_kernel(Expert
 }
 
 // out[t,:] = base[t,:] + the products of the token's slots that the call's experts hold, in
-// slot order.  One thread per 16 bytes of a slot's row; the rows of kBatch slots are under way at a time.
+// slot order.  One thread per four columns; the rows of kBatch slots are under way at a time.
 template <bool F32>
-__global__ __launch_bounds__(256) void experts_combine_kernel(const void* z, const float* factors, const int32_t* ids,
-                                                              const void* base, void* out, int T, int H, int k, int first,
-                                                              int E) {
-  constexpr int kWide = F32 ? 4 : 8;  // columns of a thread
+__global__ __launch_bounds__(256) void experts_combine_kernel(const float* z, const int32_t* ids, const void* base, void* out,
+                                                              int T, int H, int k, int first, int E) {
   constexpr int kBatch = 4;
-  const int pieces = H / kWide, blocks = shared_blocks(H);
+  const int pieces = H / 4;
   const size_t all = (size_t)T * pieces;
   for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (size_t)gridDim.x * 256) {
     const size_t t = i / pieces;
-    const int h = (int)(i - t * pieces) * kWide;
-    mma_f32x4 y[kWide / 4];
-#pragma unroll
-    for (int q = 0; q < kWide / 4; ++q) {
-      y[q] = mma_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-      if (base != nullptr) y[q] = load4<F32>(base, t * H + h + 4 * q);
-    }
+    const int h = (int)(i - t * pieces) * 4;
+    mma_f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (base != nullptr) y = load4<F32>(base, t * H + h);
     for (int j = 0; j < k; j += kBatch) {
-      mma_u32x4 row[kBatch];
-      float by[kBatch];
+      mma_f32x4 row[kBatch];
       bool is[kBatch];
 #pragma unroll
       for (int u = 0; u < kBatch; ++u)
         is[u] = j + u < k && (ids == nullptr || (unsigned)(ids[t * k + min(j + u, k - 1)] - first) < (unsigned)E);
 #pragma unroll
-      for (int u = 0; u < kBatch; ++u) {
-        const size_t slot = t * k + j + u;
-        if (is[u]) {
-          row[u] = __builtin_nontemporal_load(
-              reinterpret_cast<const mma_u32x4*>(static_cast<const unsigned char*>(z) + (slot * H + h) * (F32 ? 4 : 2)));
-          if (!F32) by[u] = factors[slot * blocks + h / kShared];
-        }
-      }
+      for (int u = 0; u < kBatch; ++u)
+        if (is[u]) row[u] = __builtin_nontemporal_load(reinterpret_cast<const mma_f32x4*>(z + (t * k + j + u) * H + h));
 #pragma unroll
-      for (int u = 0; u < kBatch; ++u) {
-        if (!is[u]) continue;
-        if constexpr (F32) {
-          y[0] += __builtin_bit_cast(mma_f32x4, row[u]);
-        } else {
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            y[w / 2][w % 2 * 2] += f16_value(row[u][w] & 0xffffu) * by[u];
-            y[w / 2][w % 2 * 2 + 1] += f16_value(row[u][w] >> 16) * by[u];
-          }
-        }
-      }
+      for (int u = 0; u < kBatch; ++u)
+        if (is[u]) y += row[u];
     }
-#pragma unroll
-    for (int q = 0; q < kWide / 4; ++q) store4<F32>(out, t * H + h + 4 * q, y[q]);
+    store4<F32>(out, t * H + h, y);
   }
 }
 
@@ -671,9 +613,7 @@ static bool are_few(int T, const ExpertArgs& a, long long rows) {
 }
 
 static size_t whole_256(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
-static size_t summands_bytes(size_t slots, int H, bool f32) {
-  return f32 ? whole_256(slots * H * 4) : whole_256(slots * H * 2) + whole_256(slots * shared_blocks(H) * 4);
-}
+static size_t summands_bytes(size_t slots, int H) { return whole_256(slots * H * 4); }
 static bool misaligned(const void* p) { return ((uintptr_t)p & 15) != 0; }
 
 // Without tables: one expert that takes every token once.
@@ -729,7 +669,7 @@ extern "C" size_t laser_experts_workspace_bytes(int32_t T, int32_t H, int32_t F,
                                                 const laser_experts_params_t* params) {
   if (check_experts(T, H, F, E, params) != LASER_OK) return 0;
   const size_t slots = (size_t)T * params->k;
-  return summands_bytes(slots, H, params->dtype == LASER_DTYPE_F32) + whole_256(slices_bytes(slots, H)) + 256;
+  return summands_bytes(slots, H) + whole_256(slices_bytes(slots, H)) + 256;
 }
 
 extern "C" int laser_experts_down(const void* act, const void* w_down, int32_t T, int32_t H, int32_t F, int32_t E,
@@ -754,7 +694,6 @@ extern "C" int laser_experts_down(const void* act, const void* w_down, int32_t T
   a.offsets = expert_offsets ? expert_offsets + params->first_expert : nullptr;
   a.weights = weights;
   a.out = workspace;
-  a.factors = reinterpret_cast<float*>(static_cast<char*>(workspace) + whole_256((size_t)T * params->k * H * 2));
   a.slots = T * params->k;
   a.k = params->k;
   a.E = E;
@@ -779,7 +718,7 @@ extern "C" int laser_experts_down(const void* act, const void* w_down, int32_t T
   }
   a.slices = f32 ? slices_of<true>(a) : slices_of<false>(a);
   if (a.slices > 1) {
-    float* const parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + summands_bytes(a.slots, H, f32));
+    float* const parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + summands_bytes(a.slots, H));
     a.out = parts;
     const hipError_t err = f32 ? launch_slices<true>(a, s) : launch_slices<false>(a, s);
     if (err != hipSuccess) return LASER_E_LAUNCH;
@@ -791,13 +730,9 @@ extern "C" int laser_experts_down(const void* act, const void* w_down, int32_t T
   }
   const hipError_t err = f32 ? launch_products<true, false>(a, s) : launch_products<false, false>(a, s);
   if (err != hipSuccess) return LASER_E_LAUNCH;
-  const size_t pieces = (size_t)T * (H / (f32 ? 4 : 8));
-  const unsigned grid = (unsigned)std::min<size_t>((pieces + 255) / 256, 1 << 16);
-  if (f32)
-    hipLaunchKernelGGL((experts_combine_kernel<true>), dim3(grid), dim3(256), 0, s, workspace, nullptr, expert_ids, base, out,
-                       T, H, params->k, params->first_expert, E);
-  else
-    hipLaunchKernelGGL((experts_combine_kernel<false>), dim3(grid), dim3(256), 0, s, workspace, a.factors, expert_ids, base,
-                       out, T, H, params->k, params->first_expert, E);
+  const unsigned grid = (unsigned)std::min<size_t>(((size_t)T * (H / 4) + 255) / 256, 1 << 16);
+  auto* const combine = f32 ? &experts_combine_kernel<true> : &experts_combine_kernel<false>;
+  hipLaunchKernelGGL(combine, dim3(grid), dim3(256), 0, s, static_cast<const float*>(workspace), expert_ids, base, out, T, H,
+                     params->k, params->first_expert, E);
   return hipGetLastError() == hipSuccess ? LASER_OK : LASER_E_LAUNCH;
 }

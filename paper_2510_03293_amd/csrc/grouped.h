@@ -67,10 +67,6 @@ __device__ __forceinline__ mma_f32x4 multiply(mma_u32x4 a, mma_u32x4 b, mma_f32x
 __device__ __forceinline__ unsigned bf16_bits(float x) {  // round to nearest even, NaN stays NaN
   return __builtin_bit_cast(unsigned short, (__bf16)x);
 }
-__device__ __forceinline__ unsigned f16_bits(float x) { return __builtin_bit_cast(unsigned short, (_Float16)x); }
-__device__ __forceinline__ float f16_value(unsigned bits) {
-  return (float)__builtin_bit_cast(_Float16, (unsigned short)bits);
-}
 __device__ __forceinline__ float bf16_value(unsigned bits) { return __builtin_bit_cast(float, bits << 16); }
 
 // Four neighbouring values of an output row, rounded to the output's type.
@@ -364,11 +360,10 @@ struct Tile {
 // beginning at that row and (wavefront's) column go, or NULL.  (Stores straight from the accumulators reach 16 rows with 32 or 64 bytes each:
 // 98304 x 2048 x 1408 in bf16 took 525 us so and 485 this way, with fp32 results 560 and 515,
 // with none 412.  They go past the caches: nobody reads them soon.)
-enum Stored { kF32, kBf16, kF16 };
-template <Stored AS, class TL, int NC, int BYTES = TL::kLdsBytes / TL::kWaves, typename VALUE, typename PLACE>
+template <bool F32, class TL, int NC, int BYTES = TL::kLdsBytes / TL::kWaves, typename VALUE, typename PLACE>
 __device__ __forceinline__ void store_tile(unsigned lds, int wave, int lane, VALUE value, PLACE place) {
   constexpr int kBytes = BYTES;
-  constexpr int kRow = NC * 16 * (AS == kF32 ? 4 : 2);      // bytes of a row
+  constexpr int kRow = NC * 16 * (F32 ? 4 : 2);      // bytes of a row
   constexpr int kFit = kBytes / (16 * kRow);
   constexpr int kPass = kFit < TL::MB ? kFit : TL::MB;      // token blocks at a time
   constexpr int kPieces = kRow / 16, kRows = 64 / kPieces;  // pieces of a row; rows per store instruction
@@ -384,14 +379,13 @@ __device__ __forceinline__ void store_tile(unsigned lds, int wave, int lane, VAL
       for (int n = 0; n < NC; ++n) {
         const mma_f32x4 v = value(n, m);
         const unsigned row = mine + ((m - m0) * 16 + tok) * kRow;
-        if constexpr (AS == kF32) {
+        if constexpr (F32) {
           *(lds_f32x4)(size_t)(row + ((n * 4 + quad) ^ (tok & kTurn)) * 16) = v;
         } else {
           mma_u32x2 b;
 #pragma unroll
           for (int i = 0; i < 2; ++i)
-            b[i] = AS == kBf16 ? bf16_bits(v[2 * i]) | bf16_bits(v[2 * i + 1]) << 16
-                               : f16_bits(v[2 * i]) | f16_bits(v[2 * i + 1]) << 16;
+            b[i] = bf16_bits(v[2 * i]) | bf16_bits(v[2 * i + 1]) << 16;
           *(lds_u32x2)(size_t)(row + ((n * 2 + (quad >> 1)) ^ (tok & kTurn)) * 16 + (quad & 1) * 8) = b;
         }
       }
@@ -404,7 +398,7 @@ __device__ __forceinline__ void store_tile(unsigned lds, int wave, int lane, VAL
       const int r = i * kRows + lane / kPieces, c = lane % kPieces;
       const int row = TL::block_row(wave, m0 + r / 16) + r % 16;
       const bool is = r < kPass * 16 && m0 + r / 16 < TL::MB;
-      to[i] = is ? static_cast<mma_u32x4*>(place(row, c * (AS == kF32 ? 4 : 8))) : nullptr;
+      to[i] = is ? static_cast<mma_u32x4*>(place(row, c * (F32 ? 4 : 8))) : nullptr;
       d[i] = read_lds(mine + min(r, kPass * 16 - 1) * kRow + (c ^ (r & kTurn)) * 16);
     }
 #pragma unroll

@@ -445,7 +445,7 @@ __device__ __forceinline__ void store_columns(const ProjectArgs& a, unsigned lds
                                               mma_f32x4 (&y)[NC][TL::MB]) {
   constexpr int kSize = OUT32 ? 4 : 2;
   if (a.N % (16 / kSize) == 0) {
-    store_tile<OUT32 ? kF32 : kBf16, TL, NC>(
+    store_tile<OUT32, TL, NC>(
         lds, wave, lane, [&](int n, int m) { return y[n][m]; },
         [&](int r, int c) -> void* {
           return r < rows && n0 + c < a.N ? static_cast<char*>(a.out) + ((size_t)(t0 + r) * a.N + n0 + c) * kSize : nullptr;
