@@ -9,7 +9,8 @@
 // added to its accumulators; a gate's few columns do all of that in one launch.
 //
 // v stays in fp32 quality up to the second product: bf16 calls hand it over in three bf16 values
-// that add up to it (8 + 8 + 8 bits), each multiplied by U on its own.
+// that add up to it (8 + 8 + 8 bits), each multiplied by U on its own.  Infinities on either side come out as in fp32:
+// see split3() and without_infinities().
 #include <algorithm>
 
 #include "../../include/laser.h"
@@ -130,13 +131,33 @@ __device__ __forceinline__ void join_wavefronts(mma_f32x4 (&acc)[B], float* part
   __syncthreads();
 }
 
-// x = hi + mid + lo, three bf16 values
+// x = hi + mid + lo, three bf16 values.  Bits are cut off, not rounded: what is above the largest bf16 stays
+// finite.  An infinity or NaN (a quiet one, as x comes from a product) is hi alone.
 __device__ __forceinline__ void split3(float x, unsigned (&piece)[3]) {
+  const bool finite = fabsf(x) < __builtin_inff();
 #pragma unroll
   for (int i = 0; i < 3; ++i) {
-    piece[i] = bf16_bits(x);
+    piece[i] = __builtin_bit_cast(unsigned, x) >> 16;
     x -= bf16_value(piece[i]);
+    if (i == 0) x = finite ? x : 0.0f;
   }
+}
+
+// An infinite entry of U is multiplied with hi alone: mid and lo of a finite inner value may be zero, and that times an
+// infinity would be NaN.  Whether any of eight bf16 values is infinite or NaN: an exponent of ones carries.
+__device__ __forceinline__ unsigned no_number(mma_u32x4 u) {
+  unsigned any = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) any |= (u[i] & 0x7f807f80u) + 0x00800080u;
+  return any & 0x80008000u;
+}
+__device__ __forceinline__ mma_u32x4 without_infinities(mma_u32x4 u) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if ((u[i] & 0x7fffu) == 0x7f80u) u[i] &= 0xffff0000u;
+    if ((u[i] & 0x7fff0000u) == 0x7f800000u) u[i] &= 0xffffu;
+  }
+  return u;
 }
 
 // v[t, r .. r + 3] as the second product reads it
@@ -390,7 +411,16 @@ __device__ __forceinline__ void add_adapters(const ProjectArgs& a, int t0, int n
     const int r = r0 + (lane >> 4) * kOwn;
     const bool in = r < a.R;
     int held = -1;  // the adapter whose rows are in u
+    bool limits = false;  // ... and whether these hold infinities or NaN (bf16)
     mma_u32x4 u[NB], ahead[kAhead][kPieces];
+    auto load_u = [&](int ad) {
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+        const int row = min(n0 + n * 16 + (lane & 15), a.N - 1);
+        u[n] = *reinterpret_cast<const mma_u32x4*>(a.a_up + (((size_t)ad * a.N + row) * a.R + (in ? r : 0)) * kSize);
+        if (!in) u[n] = mma_u32x4{0, 0, 0, 0};
+      }
+    };
 #pragma unroll
     for (int m = 0; m < MB; ++m) {
       if (m % kAhead == 0) {  // v of the next blocks, all under way at once
@@ -412,18 +442,26 @@ __device__ __forceinline__ void add_adapters(const ProjectArgs& a, int t0, int n
         todo &= ~(unsigned)__ballot(mine);
         if (ad != held) {
           held = ad;
+          load_u(ad);
+          if constexpr (!F32) {
+            unsigned any = 0;
 #pragma unroll
-          for (int n = 0; n < NB; ++n) {
-            const int row = min(n0 + n * 16 + (lane & 15), a.N - 1);
-            u[n] = *reinterpret_cast<const mma_u32x4*>(a.a_up + (((size_t)ad * a.N + row) * a.R + (in ? r : 0)) * kSize);
-            if (!in) u[n] = mma_u32x4{0, 0, 0, 0};
+            for (int n = 0; n < NB; ++n) any |= no_number(u[n]);
+            limits = __ballot(any != 0) != 0;
           }
         }
         mma_f32x4 d[NB];
 #pragma unroll
         for (int n = 0; n < NB; ++n) d[n] = mma_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        if (!F32 && limits)
+#pragma unroll
+          for (int n = 0; n < NB; ++n) u[n] = without_infinities(u[n]);
 #pragma unroll
         for (int j = kPieces - 1; j >= 0; --j) {
+          if (!F32 && j == 0 && limits) {  // (loaded again: a second set of registers would spill)
+            asm volatile("" ::: "memory");
+            load_u(ad);
+          }
           const mma_u32x4 b = mine && in ? v[j] : mma_u32x4{0, 0, 0, 0};
 #pragma unroll
           for (int n = 0; n < NB; ++n) d[n] = multiply<F32>(u[n], b, d[n]);
@@ -599,39 +637,52 @@ __global__ __launch_bounds__(512) void project_narrow_kernel(ProjectArgs a) {
             for (int i = 0; i < 4; ++i) inner[h][i] = mine && b + h < RB ? inner[h][i] * scale : 0.0f;
           }
           const int r = 16 * b + 4 * quad;
+          auto row_of = [&](int n) { return ((size_t)held[q] * a.N + min(16 * n + tok, a.N - 1)) * a.R; };
+          if constexpr (F32) {
+            const mma_f32x4 x = r < a.R ? inner[0] : mma_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-          for (int n = 0; n < 4; ++n) {
-            const size_t row = ((size_t)held[q] * a.N + min(16 * n + tok, a.N - 1)) * a.R;
-            if constexpr (F32) {
+            for (int n = 0; n < 4; ++n) {
               mma_f32x4 u = {0.0f, 0.0f, 0.0f, 0.0f};
-              if (r < a.R) u = load4<true>(a.a_up, row + r);
-              const mma_f32x4 x = r < a.R ? inner[0] : mma_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+              if (r < a.R) u = load4<true>(a.a_up, row_of(n) + r);
               d[n] = multiply<true>(__builtin_bit_cast(mma_u32x4, u), __builtin_bit_cast(mma_u32x4, x), d[n]);
-            } else {
-              const unsigned short* const up = reinterpret_cast<const unsigned short*>(a.a_up) + row;
-              mma_u32x4 u = {0, 0, 0, 0}, p[3];
+            }
+          } else {
+            mma_u32x4 u[4], p[3];
+            unsigned any = 0;
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+              const unsigned short* const up = reinterpret_cast<const unsigned short*>(a.a_up) + row_of(n);
+              u[n] = mma_u32x4{0, 0, 0, 0};
               if (r < a.R) {
                 const mma_u32x2 lo = *reinterpret_cast<const mma_u32x2*>(up + r);
-                u[0] = lo[0], u[1] = lo[1];
+                u[n][0] = lo[0], u[n][1] = lo[1];
               }
               if (b + 1 < RB && r + 16 < a.R) {
                 const mma_u32x2 hi = *reinterpret_cast<const mma_u32x2*>(up + r + 16);
-                u[2] = hi[0], u[3] = hi[1];
+                u[n][2] = hi[0], u[n][3] = hi[1];
               }
+              any |= no_number(u[n]);
+            }
 #pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                const bool in = r + 16 * h < a.R;  // (rows past the rank repeat the last one: not used)
-                unsigned s[4][3];
+            for (int h = 0; h < 2; ++h) {
+              const bool in = r + 16 * h < a.R;  // (rows past the rank repeat the last one: not used)
+              unsigned s[4][3];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) split3(in ? inner[h][i] : 0.0f, s[i]);
+              for (int i = 0; i < 4; ++i) split3(in ? inner[h][i] : 0.0f, s[i]);
 #pragma unroll
-                for (int j = 0; j < 3; ++j) {
-                  p[j][2 * h] = s[0][j] | s[1][j] << 16;
-                  p[j][2 * h + 1] = s[2][j] | s[3][j] << 16;
-                }
+              for (int j = 0; j < 3; ++j) {
+                p[j][2 * h] = s[0][j] | s[1][j] << 16;
+                p[j][2 * h + 1] = s[2][j] | s[3][j] << 16;
               }
+            }
+            const bool limits = __ballot(any != 0) != 0;
 #pragma unroll
-              for (int j = 2; j >= 0; --j) d[n] = multiply<false>(u, p[j], d[n]);
+            for (int n = 0; n < 4; ++n) {
+              mma_u32x4 rest = u[n];
+              if (limits) rest = without_infinities(rest);
+              d[n] = multiply<false>(rest, p[2], d[n]);
+              d[n] = multiply<false>(rest, p[1], d[n]);
+              d[n] = multiply<false>(u[n], p[0], d[n]);
             }
           }
         }
