@@ -463,6 +463,19 @@ def _memory_of(stream):
     return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
 
 
+def _hold(stream, used, made=()) -> None:
+    """Tensors of a call on a stream of its own may be dropped behind it: what the call uses stays until the
+    call has run, and what it allocated on its stream until the current stream, which goes on with it, is
+    through as well."""
+    if stream is None:
+        return
+    for t in used:
+        if t is not None:
+            t.record_stream(stream)
+    for t in made:
+        t.record_stream(torch.cuda.current_stream())
+
+
 class ExpertBuffers:
     """act, out and workspace of experts() for calls of one size, allocated once."""
 
@@ -503,12 +516,15 @@ def experts(hidden, w_up, w_down, routed: RouteBuffers | None, base=None, first_
         _expect("buffers.act", buffers.act, (T * k, F), dt, dev)
         _expect("buffers.out", buffers.out, (T, H), dt, dev)
     _expect_current(dev, stream, None if buffers is None else buffers.workspace)
+    tables = (None,) * 4 if routed is None else (routed.permutation, routed.expert_offsets, routed.expert_ids,
+                                                 routed.weights)
+    made = ()
     if buffers is None:
         with _memory_of(stream):
             buffers = ExpertBuffers(T, H, F, E, k, dt, device=dev)
+        made = (buffers.act, buffers.out)
+    _hold(stream, (hidden, w_up, w_down, base, *tables, buffers.act, buffers.out, buffers.workspace), made)
     params = make_experts_params(k, code, first_expert)
-    tables = (None,) * 4 if routed is None else (routed.permutation, routed.expert_offsets, routed.expert_ids,
-                                                 routed.weights)
     laser_experts_up(hidden, w_up, T, H, F, E, params, tables[0], tables[1], buffers.act, stream)
     laser_experts_down(buffers.act, w_down, T, H, F, E, params, *tables, base, buffers.out, buffers.workspace, stream)
     return buffers
@@ -549,9 +565,12 @@ def project_adapted(x, w, a_down, a_up, scales, request_offsets, request_adapter
         _expect("buffers.out", buffers.out, (T, N), out_dtype, dev)
     _expect_current(dev, stream, None if buffers is None else buffers.workspace)
     params = make_adapter_params(R, M, n, code, _CODES[out_dtype])
+    made = ()
     if buffers is None:
         with _memory_of(stream):
             buffers = ProjectBuffers(T, H, N, params, device=dev)
+        made = (buffers.out,)
+    _hold(stream, (x, w, a_down, a_up, scales, request_offsets, request_adapters, buffers.out, buffers.workspace), made)
     laser_project_adapted(x, w, T, H, N, params, a_down, a_up, scales, request_offsets, request_adapters,
                           buffers.out, buffers.workspace, stream)
     return buffers.out
