@@ -463,6 +463,14 @@ def _memory_of(stream):
     return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
 
 
+def _expect_no_gradient(**operands) -> None:
+    """The products have no backward pass: a result that would silently cut the graph is refused."""
+    if torch.is_grad_enabled():
+        for name, t in operands.items():
+            if t is not None and t.requires_grad:
+                raise ValueError(f"{name} requires a gradient and this call has none: detach it, or call under torch.no_grad()")
+
+
 def _hold(stream, used, made=()) -> None:
     """Tensors of a call on a stream of its own may be dropped behind it: what the call uses stays until the
     call has run, and what it allocated on its stream until the current stream, which goes on with it, is
@@ -494,12 +502,15 @@ def experts(hidden, w_up, w_down, routed: RouteBuffers | None, base=None, first_
             buffers: ExpertBuffers | None = None, stream=None) -> ExpertBuffers:
     """Both products of the experts behind a routing call: laser_experts_up, then laser_experts_down
     with the call's weights.  w_up [E,2F,H], w_down [E,H,F]; routed None: one expert (E = 1) for every
-    token.  The result is `out` of the returned buffers; forward only."""
+    token.  The result is `out` of the returned buffers; forward only (operands that require a gradient are
+    refused where gradients are enabled)."""
     code = _dtype_code(hidden, "hidden")
     if hidden.dim() != 2 or w_down.dim() != 3:
         raise ValueError("hidden must have 2 dimensions, w_down 3")
     (T, H), (E, _, F), dev, dt = hidden.shape, w_down.shape, hidden.device, hidden.dtype
     k = 1 if routed is None else routed.k
+    _expect_no_gradient(hidden=hidden, w_up=w_up, w_down=w_down, base=base,
+                        weights=None if routed is None else routed.weights)
     _expect("hidden", hidden, (T, H), dt, dev)
     _expect("w_up", w_up, (E, 2 * F, H), dt, dev)
     _expect("w_down", w_down, (E, H, F), dt, dev)
@@ -546,7 +557,7 @@ def project_adapted(x, w, a_down, a_up, scales, request_offsets, request_adapter
                     buffers: ProjectBuffers | None = None, stream=None) -> torch.Tensor:
     """laser_project_adapted with sizes from the tensors: x [T,H], w [N,H], a_down [M,R,H], a_up [M,N,R],
     scales [M] fp32 or None, request_offsets [requests+1] and request_adapters [requests] int32.
-    out_dtype: that of x (default) or float32.  Returns out [T,N]; forward only."""
+    out_dtype: that of x (default) or float32.  Returns out [T,N]; forward only, as experts()."""
     code = _dtype_code(x, "x")
     if x.dim() != 2 or w.dim() != 2 or a_down.dim() != 3 or request_adapters.dim() != 1:
         raise ValueError("x and w must have 2 dimensions, a_down 3, request_adapters 1")
@@ -554,6 +565,7 @@ def project_adapted(x, w, a_down, a_up, scales, request_offsets, request_adapter
     out_dtype = dt if out_dtype is None else out_dtype
     if out_dtype not in (dt, torch.float32):
         raise ValueError(f"out_dtype must be {dt} or float32, not {out_dtype}")
+    _expect_no_gradient(x=x, w=w, a_down=a_down, a_up=a_up, scales=scales)
     _expect("x", x, (T, H), dt, dev)
     _expect("w", w, (N, H), dt, dev)
     _expect("a_down", a_down, (M, R, H), dt, dev)
