@@ -13,6 +13,7 @@ import torch
 
 from paper_2510_03293_amd import binding as B
 from tests import products as P
+from tests import ways
 
 pytestmark = pytest.mark.gpu
 
@@ -41,27 +42,30 @@ def whole_numbers(T, H, F, E, k, total, first, dtype, seed):
     return act.to(P.TORCH[dtype]), w.to(P.TORCH[dtype]), perm, offs, ids, weights, base, left.to(P.TORCH[dtype]), total_sum
 
 
-# T, H, F, E, k, total, first
+# T, H, F, E, k, total, first; the way of a bf16 and of an fp32 call
 SHAPES = [
-    (1, 256, 1416, 8, 2, 8, 0),       # products with single vectors
-    (4, 136, 1032, 5, 3, 9, 2),
-    (3, 72, 9000, 2, 2, 2, 0),        # slices of the contraction axis
-    (300, 136, 1160, 3, 2, 3, 0),
-    (64, 1544, 264, 64, 6, 64, 0),    # tiles of 64 rows
-    (300, 2056, 328, 8, 2, 32, 8),
-    (2000, 1032, 520, 4, 2, 4, 0),    # tiles of 128 rows
-    (1100, 392, 1032, 1, 1, 1, 0),
-    (2600, 4360, 1160, 4, 2, 4, 0),   # tiles of 256 rows, more of them than run at once
+    (1, 256, 1416, 8, 2, 8, 0, "few", "few"),
+    (4, 136, 1032, 5, 3, 9, 2, "few", "few"),
+    (3, 72, 9000, 2, 2, 2, 0, "few", "few"),
+    (300, 136, 1160, 3, 2, 3, 0, "slices", "slices"),
+    (1100, 392, 1032, 1, 1, 1, 0, "slices", "slices"),
+    (64, 1544, 264, 64, 6, 64, 0, "64", "64"),
+    (300, 264, 328, 16, 2, 16, 0, "64", "32"),
+    (300, 2056, 328, 8, 2, 32, 8, "128", "64"),
+    (2000, 1032, 520, 4, 2, 4, 0, "128", "64"),
+    (2600, 4360, 264, 4, 2, 4, 0, "128", "64"),   # more tiles than workgroups
+    (2600, 4360, 1160, 4, 2, 4, 0, "256", "64"),  # ... of 256 rows
+    (2600, 4360, 1160, 4, 2, 12, 5, "256", "64"),  # a share of the experts
+    (5120, 2048, 1152, 1, 1, 1, 0, "256", "64"),  # ... all of them full
 ]
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "T%d_H%d_F%d_E%d_k%d" % s[:5])
 def test_sums_that_cancel_are_exact(shape, dtype):
-    T, H, F, E, k, total, first = shape
-    if dtype == F32 and T * k * H * F > 10 ** 10:
-        T = 700
+    T, H, F, E, k, total, first = shape[:7]
     act, w, perm, offs, ids, weights, base, left, whole = whole_numbers(T, H, F, E, k, total, first, dtype, 40)
+    assert ways.experts("down", T, H, F, E, k, dtype == F32, offs, first) == shape[7 if dtype == BF16 else 8]
     out = P.run_down(act, w, perm, offs, ids, weights, base, k, T, dtype, first).cpu()
     differ = int((out != left).sum())
     assert differ == 0, f"{differ} of {out.numel()} values"
