@@ -254,8 +254,8 @@ __device__ __forceinline__ void experts_tiles(const ExpertArgs& a, unsigned char
 // side by side, of so much per step and so much before and behind the steps (fitted to the figures
 // below; of a compute unit's two workgroups with 128 x 128 each has half of the steps' rate).
 //   us with 128 x 128, 256 x 256:  up of H = 2048, F = 1408, 64 experts, 2048 tokens 226, 204, 4096 tokens 354,
-//   303;  down of the same 143, 149 and 234, 212;  16 of the 64 experts, down of 1910 rows 38, 51, of 3763 rows 57,
-//   54;  8 experts, H = 4096, up of F = 2048 and 1024 tokens 114, 92, down of F = 4096 and 1500 tokens 140, 187
+//   303;  down of the same 164, 139 and 262, 239;  16 of the 64 experts, down of 1910 rows 35, 39, of 3763 rows 44,
+//   51;  8 experts, H = 4096, up of F = 2048 and 1024 tokens 114, 92, down of F = 4096 and 1500 tokens 156, 130
 struct Wide {
   using TL = Tile<false, 256, 256, 2, 4, 2>;
   static constexpr int kPerCu = 1, kStep = 25, kTile = 120, kOnce = 120;
@@ -537,12 +537,12 @@ static hipError_t launch_experts(const ExpertArgs& a, long long most, hipStream_
 // (the call's experts may be a share of the layer's): few, 64 x 128, whose weights go past the caches and are read
 // again where an expert has more than 64 rows; more, what cost_of says.  (64 x 128 and 128 x 128, up of H = 2048,
 // F = 1408, 64 experts, popularity even: 48 rows per expert 128, 142 us, 58 rows 153, 141, 66 rows 195, 145, 94 rows
-// 231, 152; skewed: 52 rows 152, 154, 58 rows 163, 154.  Down of the same, even: 48 rows 80, 88, 58 rows 93, 89,
-// 94 rows 137, 97.)  Where the rows have so few steps that 256 x 256 cannot win, 128 x 128 (8000 tokens, 2000 rows per expert, 128 x 128 and 256 x 256: down of
-// F = 320 70, 76, F = 1024 109, 116; up of H = 136 62, 80, H = 640 103, 102, H = 1024 145, 141).
+// 231, 152; skewed: 52 rows 152, 154, 58 rows 163, 154.  Down of the same, even: 48 rows 84, 86, 58 rows 93, 89,
+// 94 rows 144, 99.)  Where the rows have so few steps that 256 x 256 cannot win, 128 x 128 (8000 tokens, 2000 rows per expert, 128 x 128 and 256 x 256: down of
+// F = 320 76, 85, F = 1024 118, 125; up of H = 136 62, 80, H = 640 103, 102, H = 1024 145, 141).
 // fp32 is bound by its matrix instructions (a sixteenth of the rate) as soon as there are tiles for
 // all compute units; before that, small tiles are more of them (333 tokens, 33 experts, 516 x 212: 30 us
-// with tiles of 64 x 128, 20 with 32 x 64; 4000 tokens, 8 experts, 1024 x 1024: 333 and 391).
+// with tiles of 64 x 128, 19 with 32 x 64; 4000 tokens, 8 experts, 1024 x 1024: 354 and 425).
 constexpr int kSomeRows = 56, kWideSteps = 18;
 template <bool F32, bool UP>
 static hipError_t launch_products(const ExpertArgs& a, hipStream_t s) {
@@ -563,9 +563,9 @@ static hipError_t launch_products(const ExpertArgs& a, hipStream_t s) {
 
 // experts_down with few tiles and a long way along the contraction axis takes that in slices, at least
 // kSliceSteps steps each, as many as make kSliceWorkgroups of the tiles.  (69 tokens on 5 experts, H = 248, F = 12760:
-// 120 us in one, 18 in slices; 16 on 8, H = 512, F = 2416 29, 15; 300 on 4, H = 512, F = 1024 18.5, 15; 700 on one,
-// H = 1024, F = 2048 31, 20.)  Half of that where an expert's tiles do not share its weights, which then
-// bound the call: 500 on 4, H = 1024, F = 4096 with 256 49 us, with 512 28; 16 on 8, H = 4096, F = 14336 145, 170.
+// 119 us in one, 16 in slices; 16 on 8, H = 512, F = 2416 27, 14; 300 on 4, H = 512, F = 1024 16.4, 14; 700 on one,
+// H = 1024, F = 2048 30, 17.)  Half of that where an expert's tiles do not share its weights, which then
+// bound the call: 500 on 4, H = 1024, F = 4096 with 256 47 us, with 512 27; 16 on 8, H = 4096, F = 14336 145, 170.
 constexpr int kSliceSteps = 8, kSliceWorkgroups = 512, kSharedRows = 32;
 template <bool F32>
 using SliceTile = Tile<F32, 64, 128, 2, 2, 3>;
